@@ -3,7 +3,7 @@
 A case is a dict of plain values; `kind` says which pass it makes:
 
   adamw      grad_norm over a model's gradients and adamw_step with the clip scale, on states in 32 or 8 bits
-  quantise   quantise_fp8 of a matrix: activations in rows of 128, weights in blocks of 128 x 128
+  quantise   quantise_blocks of a matrix: activations in rows of 128, weights in blocks of 128 x 128
   logits     hidden states quantised and multiplied with an 8-bit head: what a decoding step or a prompt's scoring does
   logprobs   the log-probabilities of given tokens under that head (the generator's mu), without logits in memory
 
@@ -283,13 +283,13 @@ def run(st):
             norm = _plain_adamw(st, st["step"])
         return _adamw_outputs(st, norm if case["clip"] else None)
     if case["kind"] == "quantise":
-        q, s = L.quantise_fp8(st["x"], case["block_rows"]) if own else _plain_quantise(st["x"].float(), case["block_rows"])
+        q, s = L.quantise_blocks(st["x"], case["block_rows"]) if own else _plain_quantise(st["x"].float(), case["block_rows"])
         return dict(q=q, scale=s)
     if own:
-        Hq, Hs = L.quantise_fp8(st["H"], 1)
+        Hq, Hs = L.quantise_blocks(st["H"], 1)
         if case["kind"] == "logits":
-            return dict(z=L.logits_fp8(Hq, Hs, st["Wq"], st["Ws"], dtype=_dtype(case["out"])))
-        logp, lse = L.token_logprobs_fp8(Hq, Hs, st["Wq"], st["Ws"], st["targets"], st["mask"].reshape(-1))
+            return dict(z=L.logits_blocks(Hq, Hs, st["Wq"], st["Ws"], dtype=_dtype(case["out"])))
+        logp, lse = L.token_logprobs_blocks(Hq, Hs, st["Wq"], st["Ws"], st["targets"], st["mask"].reshape(-1))
         return dict(logp=logp, lse=lse)
     Hq, Hs = _plain_quantise(st["H"].float(), 1)
     z = _plain_dequantise(Hq, Hs, 1) @ _plain_dequantise(st["Wq"], st["Ws"], BLOCK).T
