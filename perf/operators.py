@@ -153,7 +153,7 @@ def _prepare_adamw(case, seed):
 
 
 def _plain_quantise(x, block_rows):
-    """x [R, C] -> (q float8_e4m3fn [R, C], scale float8_e8m0fnu [R or ceil(R / 128), words of four blocks])"""
+    """x [R, C] -> (q float8_e4m3fn [R, C], scale float8_e8m0fnu [C / 512 rounded up, R or ceil(R / 128), 4])"""
     R, C = x.shape
     Rb, Cb = -(-R // block_rows), -(-C // BLOCK)
     blocks = torch.zeros(Rb * block_rows, Cb * BLOCK, device=x.device)
@@ -168,12 +168,13 @@ def _plain_quantise(x, block_rows):
     q = torch.where(finite, q, torch.full_like(q, math.nan)).float().to(torch.float8_e4m3fn)
     scale = torch.full((Rb, -(-Cb // 4) * 4), 127, dtype=torch.uint8, device=x.device)
     scale[:, :Cb] = (expo + 127).to(torch.uint8)
+    scale = scale.view(Rb, -1, 4).transpose(0, 1).contiguous()
     return q.view(Rb * block_rows, Cb * BLOCK)[:R, :C].contiguous(), scale.view(torch.float8_e8m0fnu)
 
 
 def _plain_dequantise(q, scale, block_rows):
     R, C = q.shape
-    s = scale.float()[:, :-(-C // BLOCK)].repeat_interleave(BLOCK, dim=1)[:, :C]
+    s = scale.float().transpose(0, 1).flatten(1)[:, :-(-C // BLOCK)].repeat_interleave(BLOCK, dim=1)[:, :C]
     return q.float() * s.repeat_interleave(block_rows, dim=0)[:R]
 
 
@@ -345,7 +346,8 @@ def _exact_block_scale(x, block_rows):
     e = torch.where(top > 0, e.clamp(min=-127), torch.zeros_like(e))
     table = torch.ones(Rb, (Cb + 3) // 4 * 4, dtype=torch.float64, device=x.device)
     table[:, :Cb] = torch.exp2(e)
-    return table[:, :Cb].repeat_interleave(BLOCK, dim=1)[:, :C].repeat_interleave(block_rows, dim=0)[:R], table
+    full = table[:, :Cb].repeat_interleave(BLOCK, dim=1)[:, :C].repeat_interleave(block_rows, dim=0)[:R]
+    return full, table.unflatten(1, (-1, 4)).permute(1, 0, 2).contiguous()
 
 
 def _exact_adamw(case, seed):
@@ -397,7 +399,7 @@ def exact(case, seed):
         d = case["d"]
         s, _ = _exact_block_scale(st["H"], 1)
         H = (st["H"].double() / s).to(torch.float8_e4m3fn).double() * s    # the quotient is exact in bf16's bits
-        table = st["Ws"].double()
+        table = st["Ws"].double().permute(1, 0, 2).flatten(1)
         W = st["Wq"].double()
         for b in range((d + BLOCK - 1) // BLOCK):
             W[:, b * BLOCK:(b + 1) * BLOCK] *= table[:, b].repeat_interleave(BLOCK)[:W.shape[0], None]
