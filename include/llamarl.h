@@ -326,6 +326,104 @@ llamarl_status llamarl_kl_shaped_rewards(const float* rewards, const float* logp
                                          const uint8_t* mask, int64_t B, int64_t T, float lambda_kl, float* shaped,
                                          float* kl, void* stream);
 
+/*
+ * Norm of a model's gradients, over all tensors at once, and the factor that brings it down to max_norm:
+ *     norm = sqrt(sum over tensors and entries of g^2)      (squares and sums in 64 bits)
+ *     scale = max_norm / norm where norm > max_norm, 1 elsewhere; NaN where a gradient is not finite
+ * scale stays on the device and is the grad_scale of llamarl_adamw_step, which takes no step when it is not finite.
+ *
+ *   grads     HOST array [count]; an entry's arrays are on the device.  Tensors may be empty (n = 0: grad may be NULL), need the
+ *             alignment of their type only (16-byte aligned ones are read faster), and may be listed more than once
+ *   max_norm  positive; +inf: scale is 1 for any finite norm
+ *   norm      out float [1]
+ *   scale     out float [1]
+ *   ws        scratch, >= llamarl_grad_norm_workspace_bytes(count)
+ */
+typedef struct {
+  const void* grad; /* [n] of type dt */
+  int64_t n;
+  llamarl_dtype dt;
+} llamarl_gradient;
+size_t llamarl_grad_norm_workspace_bytes(int64_t count);
+llamarl_status llamarl_grad_norm(const llamarl_gradient* grads, int64_t count, float max_norm, float* norm, float* scale,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One AdamW step over all tensors of a list, in place.  With g the gradient times *grad_scale and t the step:
+ *     m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *     p = p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * in fp32 throughout.  A bf16 parameter with a master copy is the rounded master; without one it is itself widened, moved and
+ * rounded to nearest, and changes below half its last bit are lost.
+ *
+ * States in 8 bits (m_scale, v_scale not NULL): the 128 neighbouring entries 128 b .. 128 b + 127 of a tensor share one factor of
+ * each kind, and
+ *     m = m_scale[b] * e4m3(m[i])        sqrt(v) = v_scale[b] * e4m3(v[i])
+ * with factor = (largest magnitude of the block) / 448 after the step, 0 for a block below 2^-100.  p moves by the states
+ * before they are rounded.  m is rounded to nearest.  sqrt(v) changes by less than a rounding step in an update and is
+ * rounded up or down by 16 bits hashed out of (step, place in the list, entry), so that its mean is right; a v that is not zero
+ * is not rounded to zero.  Zero bytes and factors are the states of a fresh tensor.
+ *
+ *   tensors      HOST array [count]; its arrays are on the device.  Tensors of any mixture of types; empty ones (n = 0) take no
+ *                part.  Arrays need the alignment of their type only (16-byte aligned ones are faster); nothing that is written
+ *                may overlap another array of the call (INVALID_ARG).
+ *   p            HOST pointer; lr, eps, weight_decay >= 0, betas in [0, 1), step >= 1
+ *   grad_scale   device float [1] or NULL (= 1).  If it is not finite when the kernels run, no step is taken: nothing is written
+ *   lr_device    device float [1] or NULL; read when the kernels run, instead of p->lr (not checked)
+ *   step_device  device int64 [1] or NULL; the same for p->step (taken as 1 where it is less)
+ * Both let a captured graph be replayed for the next step.
+ */
+typedef struct {
+  void* param;   /* [n] of type param_dt */
+  float* master; /* [n] or NULL; bf16 parameters only */
+  const void* grad; /* [n] of type grad_dt */
+  void* m;       /* float [n], or e4m3 [n] with m_scale */
+  void* v;       /* float [n], or e4m3 [n] (the square root) with v_scale */
+  float* m_scale; /* [ceil(n / 128)] or NULL */
+  float* v_scale; /* [ceil(n / 128)] or NULL */
+  int64_t n;
+  llamarl_dtype param_dt, grad_dt;
+} llamarl_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step; /* from 1 */
+} llamarl_adamw_params;
+llamarl_status llamarl_adamw_step(const llamarl_adamw_tensor* tensors, int64_t count, const llamarl_adamw_params* p,
+                                  const float* grad_scale, const float* lr_device, const int64_t* step_device, void* stream);
+
+/*
+ * A head in 8 bits, as a generator holds it between two updates of the trainer's (Sec. 8.2, Table 3: fp8 generators beside bf16
+ * trainers).  A matrix is e4m3 (OCP, largest 448) with a power of two for each block: rows of 128 entries for
+ * activations (block_rows = 1), 128 x 128 for weights (block_rows = 128):
+ *     x[r,c] ~ q[r,c] * 2^(e - 127),   e = scale[c / 512][r / block_rows][(c / 128) % 4]
+ * scale is uint8 [ceil(cols / 512)][ceil(rows / block_rows)][4]; bytes of blocks past the last column are 127.
+ *
+ * llamarl_quantise_blocks: the smallest power of two (2^-127 at least; 1 for a block of zeros) for which no finite entry of the
+ * block exceeds 448, and x divided by it, rounded to nearest even.  Entries that are not finite become NaN.
+ *   x      in  [rows,cols] of type dt, dense; cols % 16 == 0; q: out [rows,cols] e4m3.  x and q 16-byte, scale 4-byte aligned;
+ *              none may overlap another
+ */
+llamarl_status llamarl_quantise_blocks(const void* x, int64_t rows, int64_t cols, llamarl_dtype dt, int block_rows, void* q,
+                                       uint8_t* scale, void* stream);
+
+/*
+ * Logits under such a head: z = H W^T with both operands' scales, accumulated in fp32, rounded once to z_dt.
+ *   H, H_scale  in  [N,d], d % 16 == 0, block_rows = 1;  N * d < 2^31
+ *   W, W_scale  in  [V,d], block_rows = 128;  V < 2^21
+ *   z           out [N,V] of type z_dt
+ */
+llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale, int64_t N,
+                                     int64_t d, int64_t V, llamarl_dtype z_dt, void* z, void* stream);
+
+/*
+ * llamarl_token_logprobs under such a head: the generator's mu of given tokens.  targets, mask, logp and lse as there; the logits
+ * never reach memory.
+ *   ws  scratch, >= llamarl_logprobs_blocks_workspace_bytes(N, V), which does not fall as N or V grows (0 for invalid sizes)
+ */
+size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V);
+llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale,
+                                             const int32_t* targets, const uint8_t* mask, int64_t N, int64_t d, int64_t V,
+                                             float* logp, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

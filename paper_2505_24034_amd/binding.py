@@ -28,7 +28,9 @@ EXPORTS = ("llamarl_workspace_bytes", "llamarl_last_error", "llamarl_version", "
            "llamarl_group_advantages", "llamarl_kl_shaped_rewards", "llamarl_mfma_ceiling", "llamarl_mfma_ceiling_traffic",
            "llamarl_offpolicy_loss_fwd_static", "llamarl_token_logprobs_partial", "llamarl_merge_partials",
            "llamarl_offpolicy_loss_bwd_slice", "llamarl_bwd_workspace_bytes", "llamarl_offpolicy_loss_bwd_chunked",
-           "llamarl_offpolicy_loss_bwd_device_scale")
+           "llamarl_offpolicy_loss_bwd_device_scale", "llamarl_grad_norm_workspace_bytes", "llamarl_grad_norm",
+           "llamarl_adamw_step", "llamarl_quantise_blocks", "llamarl_logits_blocks",
+           "llamarl_logprobs_blocks_workspace_bytes", "llamarl_token_logprobs_blocks")
 
 
 class LlamarlError(RuntimeError):
@@ -40,6 +42,21 @@ class LlamarlError(RuntimeError):
 class LossParams(ctypes.Structure):
     _fields_ = [("rho", ctypes.c_float), ("clip_mode", ctypes.c_int), ("eps_lo", ctypes.c_float),
                 ("eps_hi", ctypes.c_float), ("norm_mode", ctypes.c_int)]
+
+
+class Gradient(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("n", ctypes.c_int64), ("dt", ctypes.c_int)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("param_dt", ctypes.c_int), ("grad_dt", ctypes.c_int)]
+
+
+class AdamwParams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
 
 
 _lib = None
@@ -96,6 +113,20 @@ def load():
     lib.llamarl_mfma_ceiling.argtypes = [ci, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.llamarl_mfma_ceiling_traffic.restype = ci
     lib.llamarl_mfma_ceiling_traffic.argtypes = [ci, ci, vp, ctypes.c_size_t, vp, ctypes.POINTER(ctypes.c_double), vp]
+    lib.llamarl_grad_norm_workspace_bytes.restype = sz
+    lib.llamarl_grad_norm_workspace_bytes.argtypes = [i64]
+    lib.llamarl_grad_norm.restype = ci
+    lib.llamarl_grad_norm.argtypes = [ctypes.POINTER(Gradient), i64, cf, vp, vp, vp, sz, vp]
+    lib.llamarl_adamw_step.restype = ci
+    lib.llamarl_adamw_step.argtypes = [ctypes.POINTER(AdamwTensor), i64, ctypes.POINTER(AdamwParams), vp, vp, vp, vp]
+    lib.llamarl_quantise_blocks.restype = ci
+    lib.llamarl_quantise_blocks.argtypes = [vp, i64, i64, ci, ci, vp, vp, vp]
+    lib.llamarl_logits_blocks.restype = ci
+    lib.llamarl_logits_blocks.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp]
+    lib.llamarl_logprobs_blocks_workspace_bytes.restype = sz
+    lib.llamarl_logprobs_blocks_workspace_bytes.argtypes = [i64, i64]
+    lib.llamarl_token_logprobs_blocks.restype = ci
+    lib.llamarl_token_logprobs_blocks.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -321,3 +352,48 @@ def offpolicy_loss_bwd_slice(H, W_slice, targets, v0, lse, coef, grad_loss=1.0, 
     """llamarl_offpolicy_loss_bwd_slice: returns (dH_partial [N,d], dW_slice [V_slice,d])."""
     return (_native or _load_native()).offpolicy_loss_bwd_slice(H, W_slice, targets, int(v0), lse, coef, grad_loss,
                                                                 _storage(dW_dtype), ws, _handle(stream))
+
+
+def grad_norm(grads, max_norm, ws=None, stream=None):
+    """llamarl_grad_norm: a list of float32 / bfloat16 tensors -> (norm [1], scale [1]) float32 device tensors; scale is what
+    adamw_step takes as grad_scale."""
+    return (_native or _load_native()).grad_norm(grads, max_norm, ws, _handle(stream))
+
+
+def grad_norm_workspace_bytes(count):
+    return int(load().llamarl_grad_norm_workspace_bytes(count))
+
+
+STATE_BLOCK = 128
+
+
+def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, masters=None,
+               exp_avg_scales=None, exp_avg_sq_scales=None, grad_scale=None, stream=None):
+    """llamarl_adamw_step: moves every tensor of `params` (float32 or bfloat16) and its states in place.  States are float32, or
+    float8_e4m3fn with a float32 factor for each STATE_BLOCK entries in exp_avg_scales and exp_avg_sq_scales (exp_avg_sqs then
+    hold square roots).  masters: float32 copies of bfloat16 parameters.  The last three lists may hold None for a
+    tensor.  lr and step may be one-element device tensors (float32, int64), read when the kernels run; grad_scale is one
+    (float32): where it is not finite, nothing is written."""
+    (_native or _load_native()).adamw_step(params, grads, exp_avgs, exp_avg_sqs, masters, exp_avg_scales, exp_avg_sq_scales, lr,
+                                           betas[0], betas[1], eps, weight_decay, step, grad_scale, _handle(stream))
+
+
+def quantise_blocks(x, block_rows, stream=None):
+    """llamarl_quantise_blocks: x [R, C] (float32 or bfloat16) -> (q [R, C] float8_e4m3fn, scale [ceil(C / 512),
+    ceil(R / block_rows), 4] float8_e8m0fnu).  block_rows: 1 for activations, 128 for weights."""
+    return (_native or _load_native()).quantise_blocks(x, block_rows, _handle(stream))
+
+
+def logits_blocks(H, H_scale, W, W_scale, dtype=torch.float32, out=None, stream=None):
+    """llamarl_logits_blocks: H [N, d] and W [V, d] with their scales, as quantise_blocks returns them (block_rows 1 and 128)
+    -> logits [N, V] in dtype (or into `out`, in its own)."""
+    return (_native or _load_native()).logits_blocks(H, H_scale, W, W_scale, _storage(dtype), out, _handle(stream))
+
+
+def logprobs_blocks_workspace_bytes(N, V):
+    return int(load().llamarl_logprobs_blocks_workspace_bytes(N, V))
+
+
+def token_logprobs_blocks(H, H_scale, W, W_scale, targets, mask=None, ws=None, stream=None):
+    """llamarl_token_logprobs_blocks: (logp [N], lse [N]) float32 of the tokens under an 8-bit head."""
+    return (_native or _load_native()).token_logprobs_blocks(H, H_scale, W, W_scale, targets, mask, ws, _handle(stream))

@@ -1,0 +1,192 @@
+// block_entries.h -- host side of llamarl_quantise_blocks, llamarl_logits_blocks and llamarl_token_logprobs_blocks.  Part of
+// llamarl.hip.
+#pragma once
+
+namespace {
+
+typedef TileGemmBlocks<Shape256, SlabRing> Blocks256;
+typedef TileGemmBlocks<Shape128, SlabRing> Blocks128;
+
+// Which kernel a product of N tokens with V rows of W takes.
+enum BlockTile { BLOCK_FEW, BLOCK_128, BLOCK_256 };
+constexpr int FEW_RB = 2, FEW_ROWS = 16 * FEW_RB;
+BlockTile block_tile(int64_t N, int64_t V) {
+  if (N <= FEW_MAX_TOKENS) return BLOCK_FEW;
+  return tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
+}
+int block_tile_rows(BlockTile t) { return t == BLOCK_FEW ? FEW_ROWS : t == BLOCK_128 ? 128 : 256; }
+
+// As FwdWs.  The size must not fall as N or V grows: room for 128-row tiles of N tokens and for the many rows of partials of a
+// call of few.
+struct BlockWs {
+  int64_t n_pad;
+  size_t off_m, off_s, off_zt, off_rows, off_nact, total;
+};
+BlockWs block_ws(int64_t N, int64_t V) {
+  BlockWs w;
+  w.n_pad = round_up(N, 64);
+  const int64_t few = (V + FEW_ROWS - 1) / FEW_ROWS * FEW_MAX_TOKENS, many = (V + 127) / 128 * w.n_pad;
+  const int64_t plane = round_up(std::max(few, many) * 4, 256), per_token = round_up(w.n_pad * 4, 256);
+  w.off_m = 0;
+  w.off_s = (size_t)plane;
+  w.off_zt = w.off_s + (size_t)plane;
+  w.off_rows = w.off_zt + (size_t)per_token;
+  w.off_nact = w.off_rows + (size_t)per_token;
+  w.total = w.off_nact + 256;
+  return w;
+}
+
+llamarl_status check_block_matrix(int64_t rows, int64_t cols) {
+  if (rows <= 0 || cols <= 0) return fail(LLAMARL_ERR_INVALID_ARG, "sizes must be positive (got %lld, %lld)", (long long)rows, (long long)cols);
+  if (cols % 16 != 0) return fail(LLAMARL_ERR_UNSUPPORTED, "%lld columns: rows must be multiples of 16 bytes", (long long)cols);
+  if (cols >= (int64_t)1 << 22 || rows >= (int64_t)1 << 31) return fail(LLAMARL_ERR_UNSUPPORTED, "matrix too large");
+  return LLAMARL_OK;
+}
+llamarl_status check_block_head(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale, int64_t N, int64_t d, int64_t V) {
+  if (!H || !H_scale || !W || !W_scale) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
+  llamarl_status s = check_block_matrix(N, d);
+  if (s == LLAMARL_OK) s = check_block_matrix(V, d);
+  if (s != LLAMARL_OK) return s;
+  if (N * d >= (int64_t)1 << 31) return fail(LLAMARL_ERR_UNSUPPORTED, "H must be smaller than 2 GiB (its rows are gathered with 32-bit offsets)");
+  if (tile_count(N, V, 128) >= (int64_t)1 << 31 || V >= (int64_t)1 << 21) return fail(LLAMARL_ERR_UNSUPPORTED, "too many tiles or logits of a token");
+  if (!aligned16(H) || !aligned16(W)) return fail(LLAMARL_ERR_INVALID_ARG, "H and W must be 16-byte aligned");
+  if (!aligned_to(H_scale, 4) || !aligned_to(W_scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "scales must be 4-byte aligned");
+  return LLAMARL_OK;
+}
+BlockHead block_head(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale) {
+  return {static_cast<const uint8_t*>(H), static_cast<const uint8_t*>(W), reinterpret_cast<const uint32_t*>(H_scale),
+          reinterpret_cast<const uint32_t*>(W_scale)};
+}
+
+template <typename Out>
+llamarl_status launch_few(FewArgs a, hipStream_t st) {
+  const int64_t groups = (a.d + SCALE_GROUP - 1) / SCALE_GROUP;
+  a.parts = groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
+  const int64_t rows = (int64_t)(FEW_WAVES / a.parts) * FEW_ROWS;
+  a.row_blocks = (int)((a.V + rows - 1) / rows);
+  a.chunks = (int)((a.N + FEW_MAX_TOKENS - 1) / FEW_MAX_TOKENS);
+  const int64_t blocks = round_up(a.row_blocks, 8) * a.chunks;
+  if (blocks >= ((int64_t)1 << 32) / FEW_THREADS) return fail(LLAMARL_ERR_UNSUPPORTED, "too many fp32 logits for one call");
+  const auto kernel = a.N <= 16 ? k_few_tokens<FEW_RB, 1, Out> : a.N <= 32 ? k_few_tokens<FEW_RB, 2, Out> : k_few_tokens<FEW_RB, 4, Out>;
+  kernel<<<dim3((unsigned)blocks), dim3(FEW_THREADS), 0, st>>>(a);
+  HIP_TRY(hipGetLastError());
+  return LLAMARL_OK;
+}
+template <typename G>
+llamarl_status launch_block_logits(BlockLogitsArgs a, hipStream_t st) {
+  a.tiles_v = (int)((a.V + G::Shape::BM - 1) / G::Shape::BM);
+  a.tiles_t = (int)((a.N + G::Shape::BN - 1) / G::Shape::BN);
+  HIP_TRY(set_lds_if_large(k_block_logits<G>, G::LDS_BYTES));
+  k_block_logits<G><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * a.tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS),
+                      G::LDS_BYTES, st>>>(a);
+  HIP_TRY(hipGetLastError());
+  return LLAMARL_OK;
+}
+template <typename G>
+llamarl_status launch_block_partials(const FwdArgs& a, const BlockHead& x, hipStream_t st) {
+  static_assert(fwd_bytes_of<G> * G::GROUPS_PER_CU <= 160 * 1024, "LDS of a CU");
+  HIP_TRY(set_lds_if_large(k_block_partials<G>, fwd_bytes_of<G>));
+  const int64_t tiles_t = (a.N + G::Shape::BN - 1) / G::Shape::BN;
+  k_block_partials<G><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS),
+                        fwd_bytes_of<G>, st>>>(a, x.h_words, x.w_words);
+  HIP_TRY(hipGetLastError());
+  return LLAMARL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+llamarl_status llamarl_quantise_blocks(const void* x, int64_t rows, int64_t cols, llamarl_dtype dt, int block_rows, void* q,
+                                       uint8_t* scale, void* stream) {
+  if (!x || !q || !scale) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
+  if (!known(dt)) return fail(LLAMARL_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);
+  if (block_rows != 1 && block_rows != SCALE_BLOCK) return fail(LLAMARL_ERR_INVALID_ARG, "block_rows must be 1 or 128 (got %d)", block_rows);
+  const llamarl_status s = check_block_matrix(rows, cols);
+  if (s != LLAMARL_OK) return s;
+  if (!aligned16(x) || !aligned16(q)) return fail(LLAMARL_ERR_INVALID_ARG, "x and q must be 16-byte aligned");
+  if (!aligned_to(scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "scale must be 4-byte aligned");
+  const int64_t groups = (cols + SCALE_GROUP - 1) / SCALE_GROUP, scale_rows = (rows + block_rows - 1) / block_rows;
+  const int64_t x_bytes = rows * cols * (int64_t)esize(dt);
+  if (overlap(x, x_bytes, q, rows * cols) || overlap(x, x_bytes, scale, scale_rows * groups * 4) || overlap(q, rows * cols, scale, scale_rows * groups * 4))
+    return fail(LLAMARL_ERR_INVALID_ARG, "x, q and scale must not overlap");
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  QuantiseArgs a = {x, rows, cols, dt == LLAMARL_BF16, static_cast<uint8_t*>(q), reinterpret_cast<uint32_t*>(scale), (int)groups};
+  if (block_rows == 1) {
+    const int64_t blocks = (rows * groups + QUANT_THREADS / 64 - 1) / (QUANT_THREADS / 64);
+    k_quantise_rows<<<dim3((unsigned)std::min<int64_t>(blocks, (int64_t)1 << 15)), dim3(QUANT_THREADS), 0, st>>>(a);
+  } else {
+    const int64_t blocks = scale_rows * groups * 4;
+    if (blocks >= (int64_t)1 << 24) return fail(LLAMARL_ERR_UNSUPPORTED, "matrix too large");
+    k_quantise_tiles<<<dim3((unsigned)blocks), dim3(QUANT_THREADS), 0, st>>>(a);
+  }
+  HIP_TRY(hipGetLastError());
+  return LLAMARL_OK;
+}
+
+llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale, int64_t N, int64_t d,
+                                     int64_t V, llamarl_dtype z_dt, void* z, void* stream) {
+  if (!z) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
+  if (!known(z_dt)) return fail(LLAMARL_ERR_INVALID_ARG, "unknown dtype %d", (int)z_dt);
+  const llamarl_status s = check_block_head(H, H_scale, W, W_scale, N, d, V);
+  if (s != LLAMARL_OK) return s;
+  if (!aligned16(z)) return fail(LLAMARL_ERR_INVALID_ARG, "z must be 16-byte aligned");
+  const BlockHead x = block_head(H, H_scale, W, W_scale);
+  const BlockTile tile = block_tile(N, V);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  if (tile == BLOCK_FEW || z_dt == LLAMARL_F32) {
+    FewArgs f = {};
+    f.x = x; f.N = N; f.d = d; f.V = V; f.z = z;
+    return z_dt == LLAMARL_F32 ? launch_few<float>(f, st) : launch_few<uint16_t>(f, st);
+  }
+  BlockLogitsArgs a = {};
+  a.x = x; a.N = N; a.d = d; a.V = V; a.z = static_cast<uint16_t*>(z);
+  return tile == BLOCK_256 ? launch_block_logits<Blocks256>(a, st) : launch_block_logits<Blocks128>(a, st);
+}
+
+size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) { return N <= 0 || V <= 0 ? 0 : block_ws(N, V).total; }
+
+llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale,
+                                             const int32_t* targets, const uint8_t* mask, int64_t N, int64_t d, int64_t V, float* logp,
+                                             float* lse, void* ws, size_t ws_bytes, void* stream) {
+  if (!targets || !logp || !lse) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
+  llamarl_status s = check_block_head(H, H_scale, W, W_scale, N, d, V);
+  if (s != LLAMARL_OK) return s;
+  if (!aligned_to(targets, 4) || !aligned_to(logp, 4) || !aligned_to(lse, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "misaligned targets, logp or lse");
+  const BlockWs w = block_ws(N, V);
+  if (!ws || ws_bytes < w.total)
+    return fail(LLAMARL_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws ? ws_bytes : (size_t)0, w.total);
+  if (!aligned16(ws)) return fail(LLAMARL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  char* base = reinterpret_cast<char*>(ws);
+  int32_t *rows = reinterpret_cast<int32_t*>(base + w.off_rows), *n_act = reinterpret_cast<int32_t*>(base + w.off_nact);
+  const BlockTile tile = block_tile(N, V);
+  const BlockHead x = block_head(H, H_scale, W, W_scale);
+  FwdArgs a = {};
+  a.H = H; a.W = W; a.targets = targets; a.N = N; a.d = d; a.V = V;
+  a.tiles_v = (int)((V + block_tile_rows(tile) - 1) / block_tile_rows(tile));
+  a.n_pad = w.n_pad;
+  a.part_m = reinterpret_cast<float*>(base + w.off_m);
+  a.part_s = reinterpret_cast<float*>(base + w.off_s);
+  a.zt = reinterpret_cast<float*>(base + w.off_zt);
+  a.rows = rows; a.n_act = n_act;
+  k_compact_rows<<<dim3((unsigned)compact_blocks(N)), dim3(COMPACT_THREADS), 0, st>>>(
+      compact_args({0, mask, targets, nullptr, V, N, 0, rows, n_act, logp, lse, nullptr, 0.f, nullptr, nullptr}));
+  HIP_TRY(hipGetLastError());
+  if (tile == BLOCK_FEW) {
+    FewArgs f = {};
+    f.x = x; f.N = N; f.d = d; f.V = V; f.f = a;
+    s = launch_few<void>(f, st);
+  } else {
+    s = (tile == BLOCK_256 ? launch_block_partials<Blocks256> : launch_block_partials<Blocks128>)(a, x, st);
+  }
+  if (s != LLAMARL_OK) return s;
+  if (tile != BLOCK_FEW) {
+    constexpr int TOKENS = TARGET_THREADS / 64;
+    k_target_logits<<<dim3((unsigned)((N + TOKENS - 1) / TOKENS)), dim3(TARGET_THREADS), 0, st>>>(a, x);
+    HIP_TRY(hipGetLastError());
+  }
+  return launch_merge(a, logp, lse, nullptr, 0, st);
+}
+
+}  // extern "C"

@@ -224,6 +224,17 @@ __device__ __forceinline__ void logits_setup(G& g, const Args& a, const LogitsTi
                                      n_act <= TURN_COLUMNS * width ? t.tv / PATCH_ROWS_LOGITS : 0);
 }
 
+// Loops whose operands have scales of their own need the rows those belong to: row, the token row of this lane's position of
+// the tile (TokenWords).
+template <typename G, typename = void>
+struct HasScales : std::false_type {};
+template <typename G>
+struct HasScales<G, std::void_t<decltype(G::ROW_WORDS)>> : std::true_type {};
+template <typename G>
+__device__ __forceinline__ void scale_rows(G& g, const LogitsTile& t, int row) {
+  if constexpr (HasScales<G>::value) g.set_scale_rows((int64_t)t.tv * G::Shape::BM, row);
+}
+
 // f(std::integral_constant<int, column blocks of this wavefront>()): a kernel's walk over its tiles.  The wavefronts of a
 // workgroup may take different branches; all of them meet the same barriers.
 template <typename G, typename F>
@@ -281,6 +292,7 @@ __device__ __forceinline__ void fwd_tiles(const FwdArgs& a, G& g, TileSchedule<P
   int first_row = a.rows[min(cur.tt * width + Words::position(), n_act - 1)];
   logits_setup<false>(g, a, cur, n_act, grow);
   asm volatile("" : "+v"(first_row));             // waited for here, with the others, not behind the slab requests
+  scale_rows(g, cur, first_row);
 #pragma unroll
   for (int q = 0; q < G::FIRST_PARTS; ++q) issue_first<G, nb>(g, smem, q);
   bool more = sch.has_tile();
@@ -314,6 +326,7 @@ __device__ __forceinline__ void fwd_tiles(const FwdArgs& a, G& g, TileSchedule<P
     if (!last) {                                     // start the next tile's first slabs; the epilogue hides them
       cur = next;
       logits_setup<false>(g, a, cur, n_act, grow);
+      scale_rows(g, cur, word_row);
       issue_first<G, nb>(g, smem, 0);
       more = sch.has_tile();
       if (more) next.take(sch);

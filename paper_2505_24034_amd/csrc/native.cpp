@@ -19,6 +19,7 @@
 
 #include <cmath>
 #include <optional>
+#include <vector>
 
 #include "../../include/llamarl.h"
 #include "tile_rules.h"
@@ -397,6 +398,223 @@ PyObject* kl_shaped_rewards(PyObject* const* a) {
   return tuple({shaped, kl});
 }
 
+// ---- lists of tensors --------------------------------------------------------------------------------------------------
+// A Python sequence, whose items this object holds while the call runs.
+struct List {
+  PyObject* items = nullptr;            // null: None was passed
+  Py_ssize_t n = 0;
+  const char* name;
+  List(PyObject* o, const char* name_) : name(name_) {
+    if (o == Py_None) return;
+    items = PySequence_Tuple(o);
+    if (items == nullptr) throw Raised{};
+    n = PyTuple_GET_SIZE(items);
+  }
+  List(const List&) = delete;
+  ~List() { Py_XDECREF(items); }
+  PyObject* at(Py_ssize_t i) const { return items == nullptr ? Py_None : PyTuple_GET_ITEM(items, i); }
+  void same_length(Py_ssize_t count) const {
+    if (items != nullptr && n != count) invalid(std::string(name) + " must have " + std::to_string(count) + " entries");
+  }
+};
+[[noreturn]] void invalid_at(const char* name, Py_ssize_t i, const std::string& what) {
+  invalid(std::string(name) + "[" + std::to_string(i) + "] must " + what);
+}
+// An array of a list's tensor: contiguous, n entries (n < 0: any), on the list's device
+const at::Tensor& listed(const List& l, Py_ssize_t i, int64_t n, std::optional<c10::Device>& device) {
+  const at::Tensor& t = tensor(l.at(i), l.name);
+  if (!t.is_cuda() || !t.is_contiguous()) invalid_at(l.name, i, "be a contiguous device tensor");
+  if (n >= 0 && t.numel() != n) invalid_at(l.name, i, "have " + std::to_string(n) + " entries");
+  if (!device) device = t.device();
+  else if (*device != t.device()) invalid_at(l.name, i, "be on the device of the others");
+  return t;
+}
+llamarl_dtype listed_dtype(const List& l, Py_ssize_t i, const at::Tensor& t) {
+  if (t.scalar_type() == at::kBFloat16) return LLAMARL_BF16;
+  if (t.scalar_type() != at::kFloat) invalid_at(l.name, i, "be of torch.float32 or torch.bfloat16");
+  return LLAMARL_F32;
+}
+void listed_type(const List& l, Py_ssize_t i, const at::Tensor& t, at::ScalarType type, const char* type_name) {
+  if (t.scalar_type() != type) invalid_at(l.name, i, std::string("be of ") + type_name);
+}
+// written through its pointer: autograd has to see that it changed
+void bump(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// one element of the given type on `device`
+const at::Tensor& one_element(PyObject* o, at::ScalarType type, const char* type_name, const char* name, const std::optional<c10::Device>& device) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != type || !t.is_cuda() || t.numel() != 1 || (device && t.device() != *device))
+    invalid(std::string(name) + " must be one " + type_name + " on the tensors' device");
+  return t;
+}
+
+// grads, max_norm, ws, stream
+PyObject* grad_norm(PyObject* const* a) {
+  const List g(a[0], "grads");
+  if (g.n == 0) invalid("grads must hold at least one tensor");
+  const float max_norm = (float)real(a[1]);
+  std::optional<c10::Device> device;
+  std::vector<llamarl_gradient> list((size_t)g.n);
+  for (Py_ssize_t i = 0; i < g.n; ++i) {
+    const at::Tensor& t = listed(g, i, -1, device);
+    list[i] = {t.data_ptr(), t.numel(), listed_dtype(g, i, t)};
+  }
+  const at::Tensor& like = tensor(g.at(0), "grads");
+  const c10::DeviceGuard on(*device);
+  const CallStream st(a[3], like);
+  const at::Tensor norm = empty(like, {1}), scale = empty(like, {1});
+  const at::Tensor ws = workspace(a[2], llamarl_grad_norm_workspace_bytes(g.n), like);
+  check(unlocked([&] {
+    return llamarl_grad_norm(list.data(), g.n, max_norm, ptr<float>(norm), ptr<float>(scale), ptr(ws), (size_t)ws.numel(), st.handle);
+  }));
+  st.returns(norm, scale);
+  return tuple({norm, scale});
+}
+
+// params, grads, exp_avgs, exp_avg_sqs, masters, exp_avg_scales, exp_avg_sq_scales, lr, beta1, beta2, eps, weight_decay, step,
+// grad_scale, stream.  lr, step: numbers, or tensors on the device.
+PyObject* adamw_step(PyObject* const* a) {
+  const List p(a[0], "params"), g(a[1], "grads"), m(a[2], "exp_avgs"), v(a[3], "exp_avg_sqs"), masters(a[4], "masters"),
+      ms(a[5], "exp_avg_scales"), vs(a[6], "exp_avg_sq_scales");
+  for (const List* l : {&g, &m, &v, &masters, &ms, &vs}) l->same_length(p.n);
+  if (p.n > 0 && (g.items == nullptr || m.items == nullptr || v.items == nullptr)) invalid("grads, exp_avgs and exp_avg_sqs must be given");
+  std::optional<c10::Device> device;
+  std::vector<llamarl_adamw_tensor> list((size_t)p.n);
+  for (Py_ssize_t i = 0; i < p.n; ++i) {
+    llamarl_adamw_tensor& t = list[i];
+    const at::Tensor& param = listed(p, i, -1, device);
+    t = {};
+    t.n = param.numel();
+    t.param = param.data_ptr();
+    t.param_dt = listed_dtype(p, i, param);
+    const at::Tensor& grad = listed(g, i, t.n, device);
+    t.grad = grad.data_ptr();
+    t.grad_dt = listed_dtype(g, i, grad);
+    const bool bits8 = ms.at(i) != Py_None || vs.at(i) != Py_None;
+    if (bits8 && (ms.at(i) == Py_None || vs.at(i) == Py_None)) invalid_at(ms.name, i, "be given where exp_avg_sq_scales is, and only there");
+    const at::ScalarType state = bits8 ? at::kFloat8_e4m3fn : at::kFloat;
+    const char* state_name = bits8 ? "torch.float8_e4m3fn" : "torch.float32";
+    const at::Tensor &em = listed(m, i, t.n, device), &ev = listed(v, i, t.n, device);
+    listed_type(m, i, em, state, state_name);
+    listed_type(v, i, ev, state, state_name);
+    t.m = em.data_ptr();
+    t.v = ev.data_ptr();
+    if (masters.at(i) != Py_None) {
+      const at::Tensor& w = listed(masters, i, t.n, device);
+      listed_type(masters, i, w, at::kFloat, "torch.float32");
+      t.master = ptr<float>(w);
+    }
+    if (bits8) {
+      const at::Tensor &x = listed(ms, i, (t.n + 127) / 128, device), &y = listed(vs, i, (t.n + 127) / 128, device);
+      listed_type(ms, i, x, at::kFloat, "torch.float32");
+      listed_type(vs, i, y, at::kFloat, "torch.float32");
+      t.m_scale = ptr<float>(x);
+      t.v_scale = ptr<float>(y);
+    }
+  }
+  llamarl_adamw_params c = {0.0, real(a[8]), real(a[9]), real(a[10]), real(a[11]), 1};
+  const float *scale = nullptr, *lr = nullptr;
+  const int64_t* step = nullptr;
+  if (THPVariable_Check(a[7])) lr = ptr<float>(one_element(a[7], at::kFloat, "torch.float32", "lr", device));
+  else c.lr = real(a[7]);
+  if (THPVariable_Check(a[12])) step = ptr<int64_t>(one_element(a[12], at::kLong, "torch.int64", "step", device));
+  else c.step = integer(a[12]);
+  if (a[13] != Py_None) scale = ptr<float>(one_element(a[13], at::kFloat, "torch.float32", "grad_scale", device));
+  if (p.n > 0) {
+    const c10::DeviceGuard on(*device);
+    const CallStream st(a[14], tensor(p.at(0), "params"));
+    check(unlocked([&] { return llamarl_adamw_step(list.data(), p.n, &c, scale, lr, step, st.handle); }));
+    for (Py_ssize_t i = 0; i < p.n; ++i)
+      for (const List* l : {&p, &m, &v, &masters, &ms, &vs})
+        if (l->at(i) != Py_None) bump(THPVariable_Unpack(l->at(i)));
+  }
+  Py_RETURN_NONE;
+}
+
+// ---- the head in 8 bits --------------------------------------------------------------------------------------------------
+int64_t scale_groups(int64_t cols) { return (cols + 511) / 512; }
+struct Blocks {        // a matrix and its scales
+  at::Tensor q, scale;
+  Blocks(PyObject* m, const char* name, PyObject* s, const char* scale_name, int64_t block_rows) : q(tensor(m, name)), scale(tensor(s, scale_name)) {
+    if (q.scalar_type() != at::kFloat8_e4m3fn || !q.is_cuda() || !q.is_contiguous() || q.dim() != 2)
+      invalid(std::string(name) + " must be a contiguous device matrix of torch.float8_e4m3fn");
+    const int64_t rows = (q.size(0) + block_rows - 1) / block_rows;
+    if (scale.scalar_type() != at::kFloat8_e8m0fnu || !scale.is_contiguous() || scale.device() != q.device() || scale.dim() != 3 ||
+        scale.size(0) != scale_groups(q.size(1)) || scale.size(1) != rows || scale.size(2) != 4)
+      invalid(std::string(scale_name) + " must be a contiguous torch.float8_e8m0fnu tensor of shape [" +
+              std::to_string(scale_groups(q.size(1))) + ", " + std::to_string(rows) + ", 4] on the device of " + name);
+  }
+};
+struct BlockHead {
+  Blocks H, W;
+  int64_t N, d, V;
+  BlockHead(PyObject* const* a) : H(a[0], "H", a[1], "H_scale", 1), W(a[2], "W", a[3], "W_scale", 128) {
+    N = H.q.size(0);
+    d = H.q.size(1);
+    V = W.q.size(0);
+    if (W.q.size(1) != d || W.q.device() != H.q.device()) invalid("H and W must have rows of one length, on one device");
+  }
+};
+
+// x, block_rows, stream
+PyObject* quantise_blocks(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0], "x");
+  const llamarl_dtype dt = dtype_code(x);
+  need(x, x.scalar_type(), "x");
+  if (x.dim() != 2) invalid("x must be a matrix");
+  const int64_t block_rows = integer(a[1]);
+  if (block_rows != 1 && block_rows != 128) invalid("block_rows must be 1 or 128");
+  const int64_t R = x.size(0), C = x.size(1);
+  const c10::DeviceGuard on(x.device());
+  const CallStream st(a[2], x);
+  const at::Tensor q = empty(x, {R, C}, at::kFloat8_e4m3fn), scale = empty(x, {scale_groups(C), (R + block_rows - 1) / block_rows, 4}, at::kFloat8_e8m0fnu);
+  check(unlocked([&] { return llamarl_quantise_blocks(ptr(x), R, C, dt, (int)block_rows, ptr(q), ptr<uint8_t>(scale), st.handle); }));
+  st.returns(q, scale);
+  return tuple({q, scale});
+}
+
+// H, H_scale, W, W_scale, dtype code, out, stream
+PyObject* logits_blocks(PyObject* const* a) {
+  const BlockHead x(a);
+  const c10::DeviceGuard on(x.H.q.device());
+  const CallStream st(a[6], x.H.q);
+  at::Tensor z;
+  if (a[5] != Py_None) {
+    z = tensor(a[5], "out");
+    need(z, z.scalar_type(), "out");
+    if (z.dim() != 2 || z.size(0) != x.N || z.size(1) != x.V || z.device() != x.H.q.device()) invalid("out must be [N, V] on the device of H");
+  } else {
+    z = empty(x.H.q, {x.N, x.V}, integer(a[4]) == LLAMARL_BF16 ? at::kBFloat16 : at::kFloat);
+  }
+  const llamarl_dtype dt = dtype_code(z);
+  check(unlocked([&] {
+    return llamarl_logits_blocks(ptr(x.H.q), ptr<uint8_t>(x.H.scale), ptr(x.W.q), ptr<uint8_t>(x.W.scale), x.N, x.d, x.V, dt, ptr(z), st.handle);
+  }));
+  if (a[5] == Py_None) st.returns(z);
+  else bump(z);
+  return THPVariable_Wrap(z);
+}
+
+// H, H_scale, W, W_scale, targets, mask, ws, stream
+PyObject* token_logprobs_blocks(PyObject* const* a) {
+  const BlockHead x(a);
+  const at::Tensor targets = needed(a[4], at::kInt, "targets"), mask = optional(a[5], at::kByte, "mask");
+  if (targets.numel() != x.N || (mask.defined() && mask.numel() != x.N)) invalid("targets and mask must have N entries");
+  if (targets.device() != x.H.q.device() || (mask.defined() && mask.device() != x.H.q.device())) invalid("targets and mask must be on the device of H");
+  const c10::DeviceGuard on(x.H.q.device());
+  const CallStream st(a[7], x.H.q);
+  const at::Tensor logp = empty(targets, {x.N}), lse = empty(targets, {x.N});
+  const at::Tensor ws = workspace(a[6], llamarl_logprobs_blocks_workspace_bytes(x.N, x.V), targets);
+  check(unlocked([&] {
+    return llamarl_token_logprobs_blocks(ptr(x.H.q), ptr<uint8_t>(x.H.scale), ptr(x.W.q), ptr<uint8_t>(x.W.scale), ptr<int32_t>(targets),
+                                         ptr<uint8_t>(mask), x.N, x.d, x.V, ptr<float>(logp), ptr<float>(lse), ptr(ws), (size_t)ws.numel(),
+                                         st.handle);
+  }));
+  st.returns(logp, lse);
+  return tuple({logp, lse});
+}
+
 // The rules by which the library cuts and deals out its work (tile_rules.h), for tests.
 // tiles_m, tiles_n, workgroups: the tiles (row * tiles_n + column) each workgroup of a logits kernel takes, in order
 PyObject* tile_walk(PyObject* const* a) {
@@ -471,7 +689,8 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 PyMethodDef g_methods[] = {
     ENTRY(token_logprobs, 6), ENTRY(token_logprobs_partial, 8), ENTRY(merge_partials, 4), ENTRY(offpolicy_loss_fwd, 15),
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
-    ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
+    ENTRY(token_logprobs_blocks, 8), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,84 @@
+"""AdamW as a torch optimiser over the library's kernels: `llamarl_grad_norm` and `llamarl_adamw_step` in include/llamarl.h.  One
+or two launches for every 48 tensors, nothing waits for the device, and no arithmetic happens here."""
+import torch
+
+from . import binding as L
+
+
+class AdamW(torch.optim.Optimizer):
+    """params: contiguous float32 or bfloat16 tensors on the GPU, or groups of them.
+
+    state_bits      32, or 8: a quarter of the memory (binding.adamw_step says how they are held)
+    master_weights  keep a float32 copy of bfloat16 parameters, which is what moves; without it changes below half a
+                    parameter's last bit are lost
+    max_grad_norm   scale the gradients of all groups down to this norm; `grad_norm` then holds the norm before it (one
+                    element, on the device).  A norm that is not finite leaves every parameter and state as it was
+
+    lr, betas, eps, weight_decay are read from the groups at every step, as schedulers set them."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master_weights=True,
+                 max_grad_norm=None):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32 (got %r)" % (state_bits,))
+        self.state_bits, self.master_weights, self.max_grad_norm, self.grad_norm = state_bits, master_weights, max_grad_norm, None
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+
+    def _init_state(self, p):
+        s = self.state[p]
+        n = p.numel()
+        s["step"] = 0
+        if self.state_bits == 8:
+            blocks = -(-n // L.STATE_BLOCK)
+            for name in ("exp_avg", "exp_avg_sq"):
+                s[name] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+                s[name + "_scale"] = torch.zeros(blocks, device=p.device)
+        else:
+            for name in ("exp_avg", "exp_avg_sq"):
+                s[name] = torch.zeros(p.shape, device=p.device)
+        if self.master_weights and p.dtype == torch.bfloat16:
+            s["master"] = p.detach().float()
+        return s
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        """One step for every parameter that has a gradient."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        if torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise L.LlamarlError(L.ERR_UNSUPPORTED, "a captured step would repeat its step count: capture binding.adamw_step "
+                                                    "with step and lr on the device")
+        runs = {}                                         # (group, step) -> parameters and gradients
+        for i, group in enumerate(self.param_groups):
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise L.LlamarlError(L.ERR_UNSUPPORTED, "sparse gradients")
+                s = self.state[p] if self.state[p] else self._init_state(p)
+                runs.setdefault((i, s["step"] + 1), []).append((p, p.grad.contiguous()))
+        if not runs:
+            return loss
+        scale = None
+        if self.max_grad_norm is not None:
+            self.grad_norm, scale = L.grad_norm([g for pairs in runs.values() for _, g in pairs], self.max_grad_norm)
+        for (i, step), pairs in runs.items():
+            group, states = self.param_groups[i], [self.state[p] for p, _ in pairs]
+            def column(name):
+                return [s.get(name) for s in states]
+            L.adamw_step([p for p, _ in pairs], [g for _, g in pairs], column("exp_avg"), column("exp_avg_sq"), group["lr"], step,
+                         betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"], masters=column("master"),
+                         exp_avg_scales=column("exp_avg_scale"), exp_avg_sq_scales=column("exp_avg_sq_scale"), grad_scale=scale)
+            for s in states:
+                s["step"] = step
+        return loss
+
+    def load_state_dict(self, state_dict):
+        """As torch's, which would turn the states into the parameters' type."""
+        super().load_state_dict(state_dict)
+        saved = [k for group in state_dict["param_groups"] for k in group["params"]]
+        for k, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
+            if k in state_dict["state"]:
+                self.state[p] = {name: v.detach().to(p.device, copy=True) if torch.is_tensor(v) else v
+                                 for name, v in state_dict["state"][k].items()}
