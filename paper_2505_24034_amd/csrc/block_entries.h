@@ -6,15 +6,41 @@ namespace {
 
 typedef TileGemmBlocks<Shape256, SlabRing> Blocks256;
 typedef TileGemmBlocks<Shape128, SlabRing> Blocks128;
+typedef TileGemmBlocksExact<Shape128, SlabRing> BlocksExact;
 
-// Which kernel a product of N tokens with V rows of W takes.
-enum BlockTile { BLOCK_FEW, BLOCK_128, BLOCK_256 };
-constexpr int FEW_RB = 2, FEW_ROWS = 16 * FEW_RB;
-BlockTile block_tile(int64_t N, int64_t V) {
-  if (N <= FEW_MAX_TOKENS) return BLOCK_FEW;
-  return tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
+// Which kernel a product of N tokens with V rows of W takes.  us at (N, V, d), weights that are in no cache:
+//                            fp32 logits: direct / through LDS / tiles       bf16 logits, log-probs on 128-tiles : through LDS
+//   (1, 128256, 4096)          97 / 103 / 99                                   93, 110 : 103
+//   (16, 128256, 4096)        153 / 114 / 103                                  96, 111 : 114
+//   (48, 128256, 4096)          - / 134 / 113                                 104, 116 : 133, 160
+//   (1, 16032, 8192)           29 / 29 / 83                                    58,  72 : 29
+//   (16, 16032, 8192)          41 / 30 / 84                                    59,  74 : 30
+//   (48, 16032, 8192)           - / 33 / 85                                    61,  75 : 33,  45
+//   (1, 33001, 2048)           15 / 20 / 24                                    16,  27 : 20
+//   (48, 33001, 2048)           - / 28 / 25                                    17,  29 : 28,  44
+//   (16, 5003, 1024)          6.2 / 6.2 / 13.6                                7.4,  18 : 6.2
+//   (8, 1000, 8192)           8.8 / 18.7 / 81                                  32,  50 : 19
+//   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
+// So tiles of 128 rows where there is one for every CU (fp32 ones: two), below that the direct kernel for up to four tokens and for few
+// rows, the one through LDS to 64 tokens.
+enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_128, BLOCK_256 };
+BlockTile block_tile(int64_t N, int64_t V, bool exact) {
+  if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
+  // 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, bf16 logits, us at (N, V, d): (128, 128256, 4096) 127 : 123,
+  // (256, ..) 153 : 194, (300, ..) 211 : 236, (1024, ..) 524 : 667, (1900, 33001, 2048) 160 : 161, (2048, 16032, 8192) 209 : 271, (700, 8000, 1024)
+  // 22 : 15, (1041, 5003, 528) 21 : 13
+  return N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
 }
-int block_tile_rows(BlockTile t) { return t == BLOCK_FEW ? FEW_ROWS : t == BLOCK_128 ? 128 : 256; }
+// wavefronts of k_few_direct that share rows of W: as many as have a group of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192) 51 / 32 / 32 / 29,
+// (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23
+int direct_parts(int64_t d) {
+  const int64_t groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
+  return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
+}
+// rows of W that a tile of partials has
+int block_tile_rows(BlockTile t, int64_t d) {
+  return t == BLOCK_256 ? 256 : t == BLOCK_128 ? 128 : t == BLOCK_FEW ? FEW_ROWS : std::min(FEW_WAVES / direct_parts(d) * 16, 64);
+}
 
 // As FwdWs.  The size must not fall as N or V grows: room for 128-row tiles of N tokens and for the many rows of partials of a
 // call of few.
@@ -25,7 +51,7 @@ struct BlockWs {
 BlockWs block_ws(int64_t N, int64_t V) {
   BlockWs w;
   w.n_pad = round_up(N, 64);
-  const int64_t few = (V + FEW_ROWS - 1) / FEW_ROWS * FEW_MAX_TOKENS, many = (V + 127) / 128 * w.n_pad;
+  const int64_t few = (V + 15) / 16 * 64, many = (V + 127) / 128 * w.n_pad;
   const int64_t plane = round_up(std::max(few, many) * 4, 256), per_token = round_up(w.n_pad * 4, 256);
   w.off_m = 0;
   w.off_s = (size_t)plane;
@@ -58,26 +84,32 @@ BlockHead block_head(const void* H, const uint8_t* H_scale, const void* W, const
           reinterpret_cast<const uint32_t*>(W_scale)};
 }
 
-template <typename Out>
-llamarl_status launch_few(FewArgs a, hipStream_t st) {
-  const int64_t groups = (a.d + SCALE_GROUP - 1) / SCALE_GROUP;
-  a.parts = groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
-  const int64_t rows = (int64_t)(FEW_WAVES / a.parts) * FEW_ROWS;
-  a.row_blocks = (int)((a.V + rows - 1) / rows);
-  a.chunks = (int)((a.N + FEW_MAX_TOKENS - 1) / FEW_MAX_TOKENS);
-  const int64_t blocks = round_up(a.row_blocks, 8) * a.chunks;
-  if (blocks >= ((int64_t)1 << 32) / FEW_THREADS) return fail(LLAMARL_ERR_UNSUPPORTED, "too many fp32 logits for one call");
-  const auto kernel = a.N <= 16 ? k_few_tokens<FEW_RB, 1, Out> : a.N <= 32 ? k_few_tokens<FEW_RB, 2, Out> : k_few_tokens<FEW_RB, 4, Out>;
-  kernel<<<dim3((unsigned)blocks), dim3(FEW_THREADS), 0, st>>>(a);
+template <int NB, typename Out>
+llamarl_status launch_few_blocks(const FewArgs& a, hipStream_t st) {
+  HIP_TRY(set_lds_if_large(k_few_tokens<NB, Out>, FEW_LDS<NB>));
+  k_few_tokens<NB, Out><<<dim3((unsigned)((a.V + FEW_ROWS - 1) / FEW_ROWS)), dim3(FEW_THREADS), FEW_LDS<NB>, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
-template <typename G>
+template <typename Out>
+llamarl_status launch_few(FewArgs a, BlockTile tile, hipStream_t st) {
+  if (tile == BLOCK_FEW)
+    return (a.N <= 16   ? launch_few_blocks<1, Out>
+            : a.N <= 32 ? launch_few_blocks<2, Out>
+            : a.N <= 48 ? launch_few_blocks<3, Out>
+                        : launch_few_blocks<4, Out>)(a, st);
+  a.parts = direct_parts(a.d);
+  const int rows = FEW_WAVES / a.parts * 16;
+  k_few_direct<Out><<<dim3((unsigned)((a.V + rows - 1) / rows)), dim3(FEW_THREADS), 0, st>>>(a);
+  HIP_TRY(hipGetLastError());
+  return LLAMARL_OK;
+}
+template <typename G, typename Out>
 llamarl_status launch_block_logits(BlockLogitsArgs a, hipStream_t st) {
   a.tiles_v = (int)((a.V + G::Shape::BM - 1) / G::Shape::BM);
   a.tiles_t = (int)((a.N + G::Shape::BN - 1) / G::Shape::BN);
-  HIP_TRY(set_lds_if_large(k_block_logits<G>, G::LDS_BYTES));
-  k_block_logits<G><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * a.tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS),
+  HIP_TRY(set_lds_if_large(k_block_logits<G, Out>, G::LDS_BYTES));
+  k_block_logits<G, Out><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * a.tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS),
                       G::LDS_BYTES, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
@@ -132,16 +164,17 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   if (s != LLAMARL_OK) return s;
   if (!aligned16(z)) return fail(LLAMARL_ERR_INVALID_ARG, "z must be 16-byte aligned");
   const BlockHead x = block_head(H, H_scale, W, W_scale);
-  const BlockTile tile = block_tile(N, V);
+  const BlockTile tile = block_tile(N, V, z_dt == LLAMARL_F32);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (tile == BLOCK_FEW || z_dt == LLAMARL_F32) {
+  if (tile <= BLOCK_FEW) {
     FewArgs f = {};
     f.x = x; f.N = N; f.d = d; f.V = V; f.z = z;
-    return z_dt == LLAMARL_F32 ? launch_few<float>(f, st) : launch_few<uint16_t>(f, st);
+    return z_dt == LLAMARL_F32 ? launch_few<float>(f, tile, st) : launch_few<uint16_t>(f, tile, st);
   }
   BlockLogitsArgs a = {};
-  a.x = x; a.N = N; a.d = d; a.V = V; a.z = static_cast<uint16_t*>(z);
-  return tile == BLOCK_256 ? launch_block_logits<Blocks256>(a, st) : launch_block_logits<Blocks128>(a, st);
+  a.x = x; a.N = N; a.d = d; a.V = V; a.z = z;
+  if (z_dt == LLAMARL_F32) return launch_block_logits<BlocksExact, float>(a, st);
+  return tile == BLOCK_256 ? launch_block_logits<Blocks256, uint16_t>(a, st) : launch_block_logits<Blocks128, uint16_t>(a, st);
 }
 
 size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) { return N <= 0 || V <= 0 ? 0 : block_ws(N, V).total; }
@@ -160,11 +193,12 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   char* base = reinterpret_cast<char*>(ws);
   int32_t *rows = reinterpret_cast<int32_t*>(base + w.off_rows), *n_act = reinterpret_cast<int32_t*>(base + w.off_nact);
-  const BlockTile tile = block_tile(N, V);
+  const BlockTile tile = block_tile(N, V, false);
   const BlockHead x = block_head(H, H_scale, W, W_scale);
+  const int tile_rows = block_tile_rows(tile, d);
   FwdArgs a = {};
   a.H = H; a.W = W; a.targets = targets; a.N = N; a.d = d; a.V = V;
-  a.tiles_v = (int)((V + block_tile_rows(tile) - 1) / block_tile_rows(tile));
+  a.tiles_v = (int)((V + tile_rows - 1) / tile_rows);
   a.n_pad = w.n_pad;
   a.part_m = reinterpret_cast<float*>(base + w.off_m);
   a.part_s = reinterpret_cast<float*>(base + w.off_s);
@@ -173,15 +207,15 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
   k_compact_rows<<<dim3((unsigned)compact_blocks(N)), dim3(COMPACT_THREADS), 0, st>>>(
       compact_args({0, mask, targets, nullptr, V, N, 0, rows, n_act, logp, lse, nullptr, 0.f, nullptr, nullptr}));
   HIP_TRY(hipGetLastError());
-  if (tile == BLOCK_FEW) {
+  if (tile <= BLOCK_FEW) {
     FewArgs f = {};
     f.x = x; f.N = N; f.d = d; f.V = V; f.f = a;
-    s = launch_few<void>(f, st);
+    s = launch_few<void>(f, tile, st);
   } else {
     s = (tile == BLOCK_256 ? launch_block_partials<Blocks256> : launch_block_partials<Blocks128>)(a, x, st);
   }
   if (s != LLAMARL_OK) return s;
-  if (tile != BLOCK_FEW) {
+  if (tile > BLOCK_FEW) {
     constexpr int TOKENS = TARGET_THREADS / 64;
     k_target_logits<<<dim3((unsigned)((N + TOKENS - 1) / TOKENS)), dim3(TARGET_THREADS), 0, st>>>(a, x);
     HIP_TRY(hipGetLastError());

@@ -3,7 +3,7 @@
 //   k_quantise_rows, k_quantise_tiles   e4m3 and a power of two for each 1 x 128 (activations) or 128 x 128 (weights) block
 //   k_block_logits     z = H W^T of two such matrices, stored
 //   k_block_partials   the same tiles reduced to (max, sum of exp, target logit) a token: token_logprobs without logits in memory
-//   k_few_tokens       both for up to 64 tokens, bound by the bytes of W
+//   k_few_direct, k_few_tokens   both for up to 16 and 64 tokens, bound by the bytes of W
 //
 // A block's scale 2^e is the smallest power of two for which no finite entry exceeds 448 * 2^e, held as the byte e + 127;
 // q = x / 2^e is exact before it is rounded to e4m3, and so are the products with the scales.  Entries that are not finite become NaN.
@@ -123,9 +123,33 @@ struct BlockLogitsArgs {
   BlockHead x;
   int64_t N, d, V;
   int tiles_v, tiles_t;
-  uint16_t* z;             // bf16 [N][V]
+  void* z;                 // [N][V]
 };
-// A tile's accumulators to z (its first logit): four neighbouring logits of a token a store.
+// A tile's accumulators to z (its first logit): four neighbouring logits of a token a store.  fp32: buffer stores, whose lanes past
+// the matrix are put out of bounds: one offset a column is all that they keep in registers.
+template <typename S>
+__device__ __forceinline__ void store_tile(float* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT) {
+  const uint64_t p = reinterpret_cast<uint64_t>(z);
+  const auto rs = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p) |
+                                                                           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) << 32),
+                                                    (short)0, 0x7fffffff, 0x00020000);
+#pragma unroll
+  for (int j = 0; j < S::NB; ++j) {
+    const uint32_t at = lp.col(j) < rowsT ? ((uint32_t)lp.col(j) * (uint32_t)V + (uint32_t)lp.row(0, 0)) * 4u : OOB_OFFSET;
+    if (rowsV == S::BM) {                            // block-uniform
+#pragma unroll
+      for (int i = 0; i < S::MB; ++i)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4_t, acc[i][j]), rs, (int)at, 64 * i, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::MB; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[i][j][r]), rs, (int)(lp.row(i, r) < rowsV ? at : OOB_OFFSET), 64 * i + 4 * r, 0);
+    }
+    LLAMARL_FENCE();
+  }
+}
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));      // rows of z start wherever V puts them
 template <typename S>
 __device__ __forceinline__ void store_tile(uint16_t* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT) {
@@ -148,7 +172,7 @@ __device__ __forceinline__ void store_tile(uint16_t* z, int64_t V, const f32x4_t
     }
   }
 }
-template <typename G>
+template <typename G, typename Out>
 __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_block_logits(BlockLogitsArgs a) {
   typedef typename G::Shape S;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -174,11 +198,18 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_block_logit
   setup(cur);
 #pragma unroll
   for (int q = 0; q < G::FIRST_PARTS; ++q) g.issue_first(smem, q);
+  bool counted = false;
   while (true) {
     f32x4_t acc[S::MB][S::NB];
     const int64_t v0 = (int64_t)cur.tv * S::BM, t0 = (int64_t)cur.tt * S::BN;
     const int rowsV = (int)min((int64_t)S::BM, a.V - v0), rowsT = (int)min((int64_t)S::BN, a.N - t0);
-    run_tile<G, S::NB>(g, smem, acc, S::wave_col(wave_id()) * S::WAVE_N >= rowsT);
+    if (S::wave_col(wave_id()) * S::WAVE_N >= rowsT) {      // wave-uniform
+      clear(acc);
+      g.run_idle(smem);
+    } else {
+      g.run(smem, acc, counted);
+    }
+    counted = rowsV == S::BM && rowsT == S::BN;      // a store for every block of accumulators
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                    // as in fwd_tiles
     const LanePos<S> lp(tid);
@@ -193,7 +224,7 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_block_logit
       for (int q = 0; q < G::FIRST_PARTS; ++q) g.issue_first(smem, q);
     }
     LLAMARL_FENCE();
-    store_tile<S>(a.z + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT);
+    store_tile<S>(static_cast<Out*>(a.z) + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT);
     if (last) break;
   }
 }
@@ -228,176 +259,250 @@ __global__ __launch_bounds__(TARGET_THREADS) void k_target_logits(FwdArgs a, Blo
   if (lane == 0) a.zt[p] = z;
 }
 
-// ---- few tokens, and logits in fp32 ---------------------------------------------------------------------------------------------------
-// With up to 64 tokens every byte of W is used for a few products only, and the time is W's way from memory: no LDS on it, many
-// loads in flight.  A wavefront takes FEW_ROWS rows of W against all tokens, and one of KS interleaved parts of K (groups of 512
-// columns: one word of scales); the parts meet in LDS, in order.  The matrix pipe has time to spare, so the entries are widened to
-// bf16, exactly, and multiplied there: full fp32 sums (see k_target_logits), the scales on a block's sum.
-// Logits in fp32 of more tokens are taken 64 at a time: the workgroups of one part of W follow each other on one XCD, whose L2 keeps it.
+// ---- few tokens ---------------------------------------------------------------------------------------------------------------------
+// Every byte of W is used for a few products only, and the time is W's way from memory: W goes from there to the registers of the
+// one wavefront that multiplies it.  The matrix pipe has time to spare, so the entries are widened to bf16, exactly, and multiplied
+// there: full fp32 sums (see k_target_logits), the scales on a block's sum.
 struct FewArgs {
   BlockHead x;
   int64_t N, d, V;
-  int parts;               // KS: 1, 2, 4 or 8
-  int row_blocks, chunks;  // workgroups' parts of W; chunks of FEW_MAX_TOKENS tokens
+  int parts;               // k_few_direct: wavefronts that share rows of W, each with its groups of K
   void* z;                 // logits: [N][V]
-  FwdArgs f;               // log-probs: rows, n_act, targets, n_pad, part_m, part_s, zt;  tile: FEW_ROWS rows of W
+  FwdArgs f;               // log-probs: rows, n_act, targets, n_pad, part_m, part_s, zt;  tile: the rows of a workgroup
 };
-constexpr int FEW_WAVES = 8, FEW_THREADS = 64 * FEW_WAVES, FEW_MAX_TOKENS = 64;
-template <int RB>
-constexpr int FEW_PITCH = 16 * RB + 4;               // floats of a token's row in LDS
-template <int RB, int NB>
-struct FewBlock {                                    // the fragments of a block of 128 columns
-  i32x8_t w[RB], h[NB];
-};
-// eight entries of a fragment as bf16: an operand of the 16x16x32 MFMA
-__device__ __forceinline__ bf16x8_t widen(const i32x8_t& f, int quarter) {
-  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * quarter], 1.f, false),
-                 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * quarter], 1.f, true),
-                 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * quarter + 1], 1.f, false),
-                 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)f[2 * quarter + 1], 1.f, true);
-  const i32x4_t w = {__builtin_bit_cast(int, a), __builtin_bit_cast(int, b), __builtin_bit_cast(int, c), __builtin_bit_cast(int, d)};
-  return __builtin_bit_cast(bf16x8_t, w);
-}
-// NB: column blocks of 16 tokens.  Out: float or uint16_t (bf16) logits; void: partials.
-template <int RB, int NB, typename Out>
-__global__ __launch_bounds__(FEW_THREADS, 2) void k_few_tokens(FewArgs a) {
-  constexpr bool STORE = !std::is_void<Out>::value;
-  constexpr int RV = 16 * RB;
-  __shared__ float s_part[FEW_WAVES][16 * FEW_PITCH<RB>];
-  const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, g = lane >> 4;
-  const int local = blockIdx.x >> 3, row_block = local / a.chunks * 8 + (blockIdx.x & 7);
-  if (row_block >= a.row_blocks) return;             // uniform
-  const int t0 = local % a.chunks * FEW_MAX_TOKENS;
-  const int n_act = STORE ? (int)a.N : *a.f.n_act;
-  if (n_act == 0) return;                            // uniform
-  const int ks = a.parts, groups_of_rows = FEW_WAVES / ks;
-  const int kp = wave % ks;
-  const int64_t first = (int64_t)row_block * groups_of_rows * RV, row0 = first + (int64_t)(wave / ks) * RV;      // of this wavefront
-  const int64_t row0_in = min(row0, (a.V - 1) / RV * RV);            // a wavefront past the last row repeats the last ones
-  const int d = (int)a.d, blocks = (d + SCALE_BLOCK - 1) / SCALE_BLOCK, groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
-  const uint8_t* w0 = a.x.W + row0_in * a.d;
-  uint32_t woff[RB], hoff[NB];
-  int token[NB];
+constexpr int FEW_WAVES = 8, FEW_THREADS = 64 * FEW_WAVES;
+// z of up to 64 rows of W (a lane each) and a token: stored, or reduced to the tile's partials
+template <typename Out>
+__device__ __forceinline__ void few_result(const FewArgs& a, int pos, int64_t first, int rows, int64_t tile, float z) {
+  const int lane = threadIdx.x & 63;
+  const int64_t v = first + lane;
+  const bool there = lane < rows && v < a.V;
+  if (first >= a.V) return;                          // wave-uniform
+  if constexpr (std::is_void<Out>::value) {
+    float m = there ? z : -INFINITY;
 #pragma unroll
-  for (int i = 0; i < RB; ++i) woff[i] = (uint32_t)min((int64_t)(16 * i + l16), a.V - 1 - row0_in) * (uint32_t)d + 16u * g;
-#pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int at = min(t0 + 16 * j + l16, n_act - 1);
-    token[j] = STORE ? at : a.f.rows[at];
-    hoff[j] = (uint32_t)token[j] * (uint32_t)d + 16u * g;
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float base = m == -INFINITY ? 0.f : m * LOG2E;
+    const float s = wave_sum(there ? fast_exp2(fmaf(z, LOG2E, -base)) : 0.f);
+    if (lane == 0) {
+      a.f.part_m[tile * a.f.n_pad + pos] = m;
+      a.f.part_s[tile * a.f.n_pad + pos] = s;
+    }
+    if (there && v == a.f.targets[a.f.rows[pos]]) a.f.zt[pos] = z;
+  } else if (there) {
+    if constexpr (sizeof(Out) == 2) static_cast<uint16_t*>(a.z)[pos * a.V + v] = float_to_bf16_bits(z);
+    else static_cast<float*>(a.z)[pos * a.V + v] = z;
   }
+}
+template <typename Out>
+__device__ __forceinline__ int few_tokens(const FewArgs& a) {
+  if constexpr (std::is_void<Out>::value) return *a.f.n_act;
+  else return (int)a.N;
+}
+template <typename Out>
+__device__ __forceinline__ int few_token(const FewArgs& a, int at, int n_act) {      // row of H
+  const int t = min(at, n_act - 1);
+  if constexpr (std::is_void<Out>::value) return a.f.rows[t];
+  else return t;
+}
+
+// Up to 16 tokens.  A wavefront takes 16 rows of W and every parts-th group of 512 columns, all of it from memory to registers.
+constexpr int DIRECT_TOKENS = 16;
+template <typename Out>
+__global__ __launch_bounds__(FEW_THREADS, 4) void k_few_direct(FewArgs a) {
+  constexpr int PITCH = 16 + 4;                      // floats of a token's row in LDS
+  __shared__ float s_part[FEW_WAVES][DIRECT_TOKENS * PITCH];
+  const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, g = lane >> 4;
+  const int n_act = few_tokens<Out>(a);
+  if (n_act == 0) return;                            // uniform
+  const int ks = a.parts, kp = wave % ks, rows = FEW_WAVES / ks * 16;
+  const int64_t first = (int64_t)blockIdx.x * rows;
+  const int64_t row = min(first + wave / ks * 16 + l16, a.V - 1);
+  const int d = (int)a.d, groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
   const int64_t w_rows = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK;
-  const uint32_t* w_words = a.x.w_words + row0_in / SCALE_BLOCK;
-  f32x4_t acc[RB][NB];
+  const uint32_t* w_words = a.x.w_words + row / SCALE_BLOCK;         // 16 rows share it
+  const int token = few_token<Out>(a, l16, n_act);
+  const uint8_t *w = a.x.W + row * a.d, *h = a.x.H + (int64_t)token * a.d;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const i32x4_t (&x)[2], const i32x4_t (&y)[2], uint32_t ww, uint32_t hw, int b) {
+    f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  auto chunks = [](const uint8_t* p) {
-    const i32x4_t x = *reinterpret_cast<const i32x4_t*>(p), y = *reinterpret_cast<const i32x4_t*>(p + 64);
-    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  auto part_of = [&](const uint8_t* p, int k) {      // of a last block: chunks past K are zeros
-    i32x4_t x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-    if (k + 16 * g < d) x = *reinterpret_cast<const i32x4_t*>(p);
-    if (k + 64 + 16 * g < d) y = *reinterpret_cast<const i32x4_t*>(p + 64);
-    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-  };
-  auto multiply = [&](const FewBlock<RB, NB>& f, uint32_t ww, const uint32_t (&hw)[NB], int b) {
-    f32x4_t sum[RB][NB];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      bf16x8_t w[RB];
-#pragma unroll
-      for (int i = 0; i < RB; ++i) w[i] = widen(f.w[i], q);
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const bf16x8_t h = widen(f.h[j], q);
-#pragma unroll
-        for (int i = 0; i < RB; ++i) {
-          if (q == 0) sum[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          mma(w[i], h, sum[i][j]);
-        }
-      }
+    for (int c = 0; c < 2; ++c) {
+      mma(widen(x[c][0], x[c][1]), widen(y[c][0], y[c][1]), sum);
+      mma(widen(x[c][2], x[c][3]), widen(y[c][2], y[c][3]), sum);
     }
+    const float s = scale_product(ww >> 8 * b, hw >> 8 * b);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int e = exponent_of(ww, b) + exponent_of(hw[j], b);
-#pragma unroll
-      for (int i = 0; i < RB; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] += __builtin_amdgcn_ldexpf(sum[i][j][r], e);
-    }
+    for (int r = 0; r < 4; ++r) acc[r] = fmaf(sum[r], s, acc[r]);
   };
   for (int group = kp; group < groups; group += ks) {
-    const uint32_t ww = w_words[(int64_t)group * w_rows];
-    uint32_t hw[NB];
+    const uint32_t ww = w_words[(int64_t)group * w_rows], hw = a.x.h_words[(int64_t)group * a.N + token];
+    const int k = group * SCALE_GROUP + g * 16;
+    if ((group + 1) * SCALE_GROUP <= d) {            // uniform
+      i32x4_t x[4][2], y[4][2];
 #pragma unroll
-    for (int j = 0; j < NB; ++j) hw[j] = a.x.h_words[(int64_t)group * a.N + token[j]];
-    const int k = group * SCALE_GROUP;
-    if (k + SCALE_GROUP <= d) {                      // uniform
-      FewBlock<RB, NB> f[4];
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+        for (int c = 0; c < 2; ++c) {
+          x[b][c] = *reinterpret_cast<const i32x4_t*>(w + k + b * SCALE_BLOCK + c * 64);
+          y[b][c] = *reinterpret_cast<const i32x4_t*>(h + k + b * SCALE_BLOCK + c * 64);
+        }
 #pragma unroll
-        for (int i = 0; i < RB; ++i) f[b].w[i] = chunks(w0 + k + b * SCALE_BLOCK + woff[i]);
-#pragma unroll
-        for (int j = 0; j < NB; ++j) f[b].h[j] = chunks(a.x.H + k + b * SCALE_BLOCK + hoff[j]);
-      }
-#pragma unroll
-      for (int b = 0; b < 4; ++b) multiply(f[b], ww, hw, b);
+      for (int b = 0; b < 4; ++b) multiply(x[b], y[b], ww, hw, b);
     } else {
-      for (int b = 0; b < 4 && group * 4 + b < blocks; ++b) {
-        FewBlock<RB, NB> f;
-        const int kb = k + b * SCALE_BLOCK;
+      for (int b = 0; b < 4 && group * SCALE_GROUP + b * SCALE_BLOCK < d; ++b) {
+        i32x4_t x[2], y[2];
 #pragma unroll
-        for (int i = 0; i < RB; ++i) f.w[i] = part_of(w0 + kb + woff[i], kb);
-#pragma unroll
-        for (int j = 0; j < NB; ++j) f.h[j] = part_of(a.x.H + kb + hoff[j], kb);
-        multiply(f, ww, hw, b);
+        for (int c = 0; c < 2; ++c) {
+          const int at = k + b * SCALE_BLOCK + c * 64, in = min(at, d - 16);
+          x[c] = *reinterpret_cast<const i32x4_t*>(w + in);
+          y[c] = *reinterpret_cast<const i32x4_t*>(h + in);
+          if (at >= d) x[c] = y[c] = i32x4_t{0, 0, 0, 0};            // past K
+        }
+        multiply(x, y, ww, hw, b);
       }
     }
   }
-  // 16 tokens at a time: every wavefront's part to LDS, then RV lanes a token and group of rows sum them in order
+  *reinterpret_cast<f32x4_t*>(&s_part[wave][l16 * PITCH + 4 * g]) = acc;
+  __syncthreads();
+  // a wavefront sums 64 rows of a token at a time, in the order of their parts
+  const int per_token = (rows + 63) / 64;            // 1 or 2; rows are 16, 32, 64 or 128
+  for (int at = wave; at < DIRECT_TOKENS * per_token; at += FEW_WAVES) {
+    const int pos = at / per_token, sub = at - pos * per_token;
+    if (pos >= n_act) break;                         // wave-uniform
+    const int v = sub * 64 + lane;
+    float z = 0.f;
+    if (v < rows)
+      for (int p = 0; p < ks; ++p) z += s_part[(v >> 4) * ks + p][pos * PITCH + (v & 15)];
+    few_result<Out>(a, pos, first + sub * 64, min(rows, 64), (int64_t)blockIdx.x * per_token + sub, z);
+  }
+}
+
+// Up to 64 tokens.  A workgroup takes 64 rows of W: a wavefront 16 rows and one half of the groups; the halves meet in LDS at the end, in
+// order.  The tokens' part of a group is brought to LDS once for the four wavefronts of a half: read by each of them from L2 it was more
+// traffic than W's (48 tokens 217 - 250 us of a 128256 x 4096 head, 134 here).  W's registers are loaded again, for the next group, as soon as a
+// block is multiplied.  Workgroups start at groups of their own: see SlabOrder.
+constexpr int FEW_TOKENS = 64, FEW_ROWS = 64;
+constexpr int FEW_PITCH = FEW_ROWS + 4;              // floats of a token's row in LDS
+template <int NB>
+constexpr int FEW_SLAB = NB * 16 * SLAB_ROW_BYTES;   // a block of 128 columns of the tokens
+template <int NB>
+constexpr int FEW_LDS = 2 * 2 * 4 * FEW_SLAB<NB>;
+// NB: column blocks of 16 tokens.  Out: float or uint16_t (bf16) logits; void: partials.
+template <int NB, typename Out>
+__global__ __launch_bounds__(FEW_THREADS, NB == 1 ? 4 : 2) void k_few_tokens(FewArgs a) {
+  constexpr int ITEMS = 2 * NB;                      // 16-byte chunks of the tokens' part of a group that a thread brings
+  extern __shared__ __attribute__((aligned(1024))) char smem[];      // [half][buffer][block][token][128 bytes, swizzled]
+  const int lane = threadIdx.x & 63, wave = wave_id(), l16 = lane & 15, g = lane >> 4;
+  const int n_act = few_tokens<Out>(a);
+  if (n_act == 0) return;                            // uniform
+  const int half = wave >> 2;
+  const int64_t first = (int64_t)blockIdx.x * FEW_ROWS;
+  const int64_t row = min(first + (wave & 3) * 16 + l16, a.V - 1);   // of this lane; past the last row the last again
+  const int d = (int)a.d, groups = (d + SCALE_GROUP - 1) / SCALE_GROUP, turns = (groups + 1) / 2;
+  const uint8_t* w = a.x.W + row * a.d;
+  const int64_t w_rows = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK;
+  const uint32_t* w_words = a.x.w_words + first / SCALE_BLOCK;
+  int token[NB];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    if (t0 + 16 * j >= n_act) break;                 // uniform
-    if (j > 0) __syncthreads();
+  for (int j = 0; j < NB; ++j) token[j] = few_token<Out>(a, 16 * j + l16, n_act);
+  const int in_half = threadIdx.x & 255, h_chunk = in_half % 32 * 16;
+  uint32_t h_from[ITEMS];                            // chunk in_half % 32 of token 8 it + in_half / 32
 #pragma unroll
-    for (int i = 0; i < RB; ++i)
-      *reinterpret_cast<f32x4_t*>(&s_part[wave][l16 * FEW_PITCH<RB> + 16 * i + 4 * g]) = acc[i][j];
-    __syncthreads();
-    for (int at = threadIdx.x; at < groups_of_rows * 16 * RV; at += FEW_THREADS) {      // whole wavefronts
-      const int v = at % RV, n = at / RV % 16, rg = at / (RV * 16);
-      float z = 0.f;
-      for (int p = 0; p < ks; ++p) z += s_part[rg * ks + p][n * FEW_PITCH<RB> + v];
-      const int64_t row = first + (int64_t)rg * RV + v;
-      const int pos = t0 + 16 * j + n;
-      if constexpr (STORE) {
-        if (pos < n_act && row < a.V) {
-          if constexpr (sizeof(Out) == 2) static_cast<uint16_t*>(a.z)[pos * a.V + row] = float_to_bf16_bits(z);
-          else static_cast<float*>(a.z)[pos * a.V + row] = z;
-        }
-      } else {
-        const bool there = row < a.V;
-        float m = there ? z : -INFINITY;
+  for (int it = 0; it < ITEMS; ++it) h_from[it] = (uint32_t)few_token<Out>(a, 8 * it + in_half / 32, n_act) * (uint32_t)d;
+  const int start = (int)(blockIdx.x % (unsigned)turns);
+  auto group_of = [&](int turn) {                    // may be one past the last in the second half
+    const int t = turn + start;
+    return 2 * (t >= turns ? t - turns : t) + half;
+  };
+  i32x4_t x[4][2], y[ITEMS];
+  uint32_t ww, hw[NB], ww_next = 0, hw_next[NB];
+  // past K: from a place that exists; made zeros where they are used, a load is not waited for where it is asked for
+  auto w_at = [&](int group, int b, int c) { return group * SCALE_GROUP + b * SCALE_BLOCK + c * 64 + g * 16; };
+  auto load_w = [&](int group, int b) {
 #pragma unroll
-        for (int o = RV / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-        const float base = m == -INFINITY ? 0.f : m * LOG2E;
-        float s = there ? fast_exp2(fmaf(z, LOG2E, -base)) : 0.f;
+    for (int c = 0; c < 2; ++c) x[b][c] = *reinterpret_cast<const i32x4_t*>(w + min(w_at(group, b, c), d - 16));
+  };
+  auto load_h = [&](int group) {
+    const uint32_t at = (uint32_t)min(group * SCALE_GROUP + h_chunk, d - 16);
 #pragma unroll
-        for (int o = RV / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-        if (pos < n_act && first + (int64_t)rg * RV < a.V) {
-          const int64_t tile = (first + (int64_t)rg * RV) / RV;
-          if (v == 0) {
-            a.f.part_m[tile * a.f.n_pad + pos] = m;
-            a.f.part_s[tile * a.f.n_pad + pos] = s;
-          }
-          if (there && row == a.f.targets[a.f.rows[pos]]) a.f.zt[pos] = z;
+    for (int it = 0; it < ITEMS; ++it) y[it] = *reinterpret_cast<const i32x4_t*>(a.x.H + h_from[it] + at);
+  };
+  auto load_words = [&](int group, uint32_t& rw, uint32_t (&cw)[NB]) {
+    const int64_t at = min(group, groups - 1);
+    rw = w_words[at * w_rows];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) cw[j] = a.x.h_words[at * a.N + token[j]];
+  };
+  auto bring = [&](int group, int buffer) {
+    const bool past = group * SCALE_GROUP + h_chunk >= d;
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int t = 8 * it + in_half / 32, b = in_half % 32 / 8, c = in_half % 8;
+      if (past) y[it] = i32x4_t{0, 0, 0, 0};
+      *reinterpret_cast<i32x4_t*>(smem + ((half * 2 + buffer) * 4 + b) * FEW_SLAB<NB> + t * SLAB_ROW_BYTES + (c ^ swizzle(t)) * 16) = y[it];
+    }
+  };
+  f32x4_t acc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  load_h(group_of(0));
+  load_words(group_of(0), ww, hw);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) load_w(group_of(0), b);
+  bring(group_of(0), 0);
+  __syncthreads();
+  for (int turn = 0; turn < turns; ++turn) {
+    const bool more = turn + 1 < turns;              // uniform
+    const int now = group_of(turn), next = group_of(more ? turn + 1 : turn);
+    load_h(next);
+    load_words(next, ww_next, hw_next);
+    const char* st = smem + (half * 2 + (turn & 1)) * 4 * FEW_SLAB<NB> + l16 * SLAB_ROW_BYTES;
+    if ((now + 1) * SCALE_GROUP > d) {               // wave-uniform
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          if (w_at(now, b, c) >= d) x[b][c] = i32x4_t{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      f32x4_t sum[NB];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8_t w0 = widen(x[b][c][0], x[b][c][1]), w1 = widen(x[b][c][2], x[b][c][3]);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const i32x4_t v = *reinterpret_cast<const i32x4_t*>(st + b * FEW_SLAB<NB> + j * BLOCK_BYTES + ((4 * c + g) ^ swizzle(l16)) * 16);
+          if (c == 0) sum[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          mma(w0, widen(v[0], v[1]), sum[j]);
+          mma(w1, widen(v[2], v[3]), sum[j]);
         }
       }
+      load_w(next, b);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float s = scale_product(ww >> 8 * b, hw[j] >> 8 * b);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[j][r] = fmaf(sum[j][r], s, acc[j][r]);
+      }
     }
+    ww = ww_next;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) hw[j] = hw_next[j];
+    if (more) bring(next, (turn + 1) & 1);
+    __syncthreads();
+  }
+  // 16 tokens at a time: both halves to LDS, then a wavefront a token sums them over the 64 rows
+  float(*part)[16 * FEW_PITCH] = reinterpret_cast<float(*)[16 * FEW_PITCH]>(smem);
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    if (16 * j >= n_act) break;                      // uniform
+    if (j > 0) __syncthreads();
+    *reinterpret_cast<f32x4_t*>(&part[half][l16 * FEW_PITCH + 16 * (wave & 3) + 4 * g]) = acc[j];
+    __syncthreads();
+    for (int n = wave; n < 16 && 16 * j + n < n_act; n += FEW_WAVES)         // wave-uniform
+      few_result<Out>(a, 16 * j + n, first, FEW_ROWS, blockIdx.x, part[0][n * FEW_PITCH + lane] + part[1][n * FEW_PITCH + lane]);
   }
 }
 

@@ -61,9 +61,9 @@ struct ScaleWords {
   }
 };
 
-// Shape256: 256 x 256, one workgroup a CU.  Shape128: 128 x 128, two.
+// What the loops share: operand streams, scale words, stages.  Shape256: 256 x 256, one workgroup a CU.  Shape128: 128 x 128, two.
 template <typename S_, typename Order_>
-struct TileGemmBlocks {
+struct BlockStreams {
   typedef FP8 Type;
   typedef S_ Shape;
   typedef i32x8_t frag_t;
@@ -159,12 +159,49 @@ struct TileGemmBlocks {
   }
   __device__ __forceinline__ static uint32_t word(const char* p) { return *reinterpret_cast<const uint32_t*>(p); }
   __device__ __forceinline__ static uint32_t pick(uint32_t w, int k0) { return w >> ((k0 / SCALE_BLOCK & 3) * 8); }
+  __device__ __forceinline__ static Addresses addresses() {
+    const int lane = threadIdx.x & 63, wave = wave_id(), g = lane >> 4, l16 = lane & 15, sw = swizzle(l16);
+    Addresses ad;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      ad.a[c] = (Shape::wave_row(wave) * Shape::WAVE_M + l16) * SLAB_ROW_BYTES + (((4 * c + g) ^ sw) * 16);
+      ad.b[c] = Shape::SLAB_A_BYTES + (Shape::wave_col(wave) * Shape::WAVE_N + l16) * SLAB_ROW_BYTES + (((4 * c + g) ^ sw) * 16);
+    }
+    ad.cw = COL_WORDS + (Shape::wave_col(wave) * Shape::WAVE_N + l16) * 4;
+    ad.rw = ROW_WORDS + wave * 256 + lane * 4;
+    return ad;
+  }
+};
 
+// On the 8-bit matrix pipe.
+template <typename S_, typename Order_>
+struct TileGemmBlocks : BlockStreams<S_, Order_> {
+  typedef BlockStreams<S_, Order_> Base;
+  typedef S_ Shape;
+  typedef typename Base::Addresses Addresses;
+  typedef typename Base::Scales Scales;
+  typedef i32x8_t frag_t;
+  using Base::K;
+  using Base::MB;
+  using Base::NB;
+  using Base::la;
+  using Base::lb;
+  using Base::frag_a;
+  using Base::frag_b;
+  using Base::issue_words;
+  using Base::pick;
+  using Base::slab_k;
+  using Base::word;
+
+  // Slot of the n-th load of a slab (the words' are the last, together), after TB.  Where no fragment is read, then every other slot: against
+  // a load in each slot from TB on, 9216 tokens of a 128256 x 4096 head 3.66 -> 3.56 ms, (2048, 16032, 8192) 210 -> 202 us; two loads a
+  // slot 3.71 ms; a barrier two or three slots later 3.61 - 3.66.
+  __device__ __forceinline__ static constexpr int load_slot(int n) { return n < 4 ? n : n < 8 ? 2 * n - 4 : 11; }
   // One slab.  MB x 4 slots: pairs of row blocks, eight slots a pair, two a column block, the row operand snaking.  A fragment is
   // eight registers, so four row fragments are held, the pair's and the next's, and four column fragments once:
   //   - a pair's row fragments are read at the start of the pair before, into the registers of the one before that;
   //   - the slab's own reads so end at the start of its last pair but one; there is the barrier (TB), and behind it the slab after next
-  //     is requested, a load a slot;
+  //     is requested (load_slot);
   //   - the next slab's column block j is read when the last pair is done with this one's, seven slots ahead of its use, and
   //     its first row pair at the start of the last pair.
   // row_next: the rows' word of the next slab, whose byte is picked when this slab is done.
@@ -172,8 +209,8 @@ struct TileGemmBlocks {
   __device__ __forceinline__ void step(frag_t (&a)[4], frag_t (&b)[NB], Scales& sc, f32x4_t (&acc)[MB][NB], char* cur, const char* nxt,
                                        const Addresses& ad, int k_cur, int k_fetch) const {
     constexpr int PAIRS = MB / 2, LAST = 8 * (PAIRS - 1), TB = LAST - 5;
-    constexpr int LA = LoaderA::ITERS, LB = LoaderB::ITERS;
-    static_assert(TB + LA + LB + 1 < 8 * PAIRS, "every load has a slot");
+    constexpr int LA = Base::LoaderA::ITERS, LB = Base::LoaderB::ITERS;
+    static_assert(LA + LB == 8 && TB + 1 + load_slot(8) < 8 * PAIRS, "every load has a slot");
     const int lane = threadIdx.x & 63, wave = wave_id();
     i32x4_t ra, rb;
     if (FETCH) {
@@ -206,29 +243,26 @@ struct TileGemmBlocks {
         }
       }
       LLAMARL_FENCE();
-      if (FETCH && t > TB && t <= TB + LA + LB + 1) {
-        const int n = t - TB - 1;
-        if (n < LA) la.issue_one(ra, cur, n, k_fetch, K, wave, lane);
-        else if (n < LA + LB) lb.issue_one(rb, cur + Shape::SLAB_A_BYTES, n - LA, k_fetch, K, wave, lane);
-        else issue_words(cur, k_fetch);
-        LLAMARL_FENCE();
+      if (FETCH) {
+#pragma unroll
+        for (int n = 0; n <= LA + LB; ++n)
+          if (t == TB + 1 + load_slot(n)) {
+            if (n < LA) la.issue_one(ra, cur, n, k_fetch, K, wave, lane);
+            else if (n < LA + LB) lb.issue_one(rb, cur + Shape::SLAB_A_BYTES, n - LA, k_fetch, K, wave, lane);
+            else issue_words(cur, k_fetch);
+            LLAMARL_FENCE();
+          }
       }
     }
     if (BAR) sc.row = row_next;
   }
-  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB]) {
-    const int lane = threadIdx.x & 63, wave = wave_id();
-    const int nk = slabs();
-    const int g = lane >> 4, l16 = lane & 15, sw = swizzle(l16);
-    Addresses ad;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      ad.a[c] = (Shape::wave_row(wave) * Shape::WAVE_M + l16) * SLAB_ROW_BYTES + (((4 * c + g) ^ sw) * 16);
-      ad.b[c] = Shape::SLAB_A_BYTES + (Shape::wave_col(wave) * Shape::WAVE_N + l16) * SLAB_ROW_BYTES + (((4 * c + g) ^ sw) * 16);
-    }
-    ad.cw = COL_WORDS + (Shape::wave_col(wave) * Shape::WAVE_N + l16) * 4;
-    ad.rw = ROW_WORDS + wave * 256 + lane * 4;
-    wait_vmcnt0();
+  // counted (wave-uniform): MB * NB stores of the previous tile, and no other vector-memory operation, were issued after the first
+  // slabs were requested.  They drain under the first slab.
+  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {
+    const int nk = this->slabs();
+    const Addresses ad = Base::addresses();
+    if (counted) wait_vmcnt<MB * NB>();
+    else wait_vmcnt0();
     __syncthreads();
     frag_t a[4], b[NB];
     Scales sc;
@@ -245,7 +279,7 @@ struct TileGemmBlocks {
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     LLAMARL_FENCE();
-    char *s = smem, *o = smem + STAGE;
+    char *s = smem, *o = smem + Base::STAGE;
     for (int kt = 0; kt < nk - 1; ++kt) {
       step<true, true>(a, b, sc, acc, s, o, ad, slab_k(kt), slab_k(kt + 2));
       char* x = s;
@@ -253,6 +287,93 @@ struct TileGemmBlocks {
       o = x;
     }
     step<false, false>(a, b, sc, acc, s, o, ad, slab_k(nk - 1), 0);
+  }
+};
+
+// eight entries of a fragment as bf16, exactly: an operand of the 16x16x32 MFMA
+__device__ __forceinline__ bf16x8_t widen(int lo, int hi) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, 1.f, true),
+                 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)hi, 1.f, true);
+  const i32x4_t w = {__builtin_bit_cast(int, a), __builtin_bit_cast(int, b), __builtin_bit_cast(int, c), __builtin_bit_cast(int, d)};
+  return __builtin_bit_cast(bf16x8_t, w);
+}
+// 2^(sum of two scales), the ends of fp32's range for what lies beyond
+__device__ __forceinline__ float scale_product(uint32_t a, uint32_t b) {
+  return __builtin_amdgcn_ldexpf(1.f, min((int)(a & 0xffu) + (int)(b & 0xffu) - 254, 127));
+}
+
+// The same streams with fp32 sums: fragments are widened to bf16 and multiplied there, a block's sum is scaled into the accumulators.  128
+// widenings and 64 fused multiply-adds beside 64 MFMAs of 16 cycles a wavefront and slab: the vector instructions of one wavefront run
+// under the other's MFMAs.
+template <typename S_, typename Order_>
+struct TileGemmBlocksExact : BlockStreams<S_, Order_> {
+  typedef BlockStreams<S_, Order_> Base;
+  typedef S_ Shape;
+  typedef typename Base::Addresses Addresses;
+  using Base::K;
+  using Base::MB;
+  using Base::NB;
+  using Base::slab_k;
+  using Base::word;
+  static_assert(MB == 4, "sums of a slab beside the accumulators");
+
+  __device__ __forceinline__ static void slab(const char* st, const Addresses& ad, f32x4_t (&acc)[MB][NB], int k0) {
+    f32x4_t sum[MB][NB];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      i32x4_t x[MB], y[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) y[j] = *reinterpret_cast<const i32x4_t*>(st + ad.b[c] + j * BLOCK_BYTES);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const i32x4_t*>(st + ad.a[c] + i * BLOCK_BYTES);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {                  // 32 of a block's columns: eight entries a lane
+        bf16x8_t b[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[j] = widen(y[j][2 * h], y[j][2 * h + 1]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          const bf16x8_t a = widen(x[i][2 * h], x[i][2 * h + 1]);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) {
+            if (c == 0 && h == 0) sum[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            mma(a, b[j], sum[i][j]);
+          }
+        }
+      }
+    }
+    const uint32_t row = Base::pick(word(st + ad.rw), k0);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const float s = scale_product(row, Base::pick(word(st + ad.cw + j * 64), k0));
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(sum[i][j][r], s, acc[i][j][r]);
+    }
+  }
+  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {      // see TileGemmBlocks::run
+    const int nk = this->slabs();
+    const Addresses ad = Base::addresses();
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (counted) wait_vmcnt<MB * NB>();
+    else wait_vmcnt0();
+    __syncthreads();
+    char *s = smem, *o = smem + Base::STAGE;
+    for (int kt = 0; kt < nk - 1; ++kt) {
+      slab(s, ad, acc, slab_k(kt));
+      wait_vmcnt0();                                 // the next slab, asked for one slab ago
+      __syncthreads();
+      this->issue_slab(s, kt + 2);
+      char* x = s;
+      s = o;
+      o = x;
+    }
+    slab(s, ad, acc, slab_k(nk - 1));
   }
 };
 
