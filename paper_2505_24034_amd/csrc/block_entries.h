@@ -143,15 +143,12 @@ llamarl_status llamarl_quantise_blocks(const void* x, int64_t rows, int64_t cols
   if (overlap(x, x_bytes, q, rows * cols) || overlap(x, x_bytes, scale, scale_rows * groups * 4) || overlap(q, rows * cols, scale, scale_rows * groups * 4))
     return fail(LLAMARL_ERR_INVALID_ARG, "x, q and scale must not overlap");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  QuantiseArgs a = {x, rows, cols, dt == LLAMARL_BF16, static_cast<uint8_t*>(q), reinterpret_cast<uint32_t*>(scale), (int)groups};
-  if (block_rows == 1) {
-    const int64_t blocks = (rows * groups + QUANT_THREADS / 64 - 1) / (QUANT_THREADS / 64);
-    k_quantise_rows<<<dim3((unsigned)std::min<int64_t>(blocks, (int64_t)1 << 15)), dim3(QUANT_THREADS), 0, st>>>(a);
-  } else {
-    const int64_t blocks = scale_rows * groups * 4;
-    if (blocks >= (int64_t)1 << 24) return fail(LLAMARL_ERR_UNSUPPORTED, "matrix too large");
-    k_quantise_tiles<<<dim3((unsigned)blocks), dim3(QUANT_THREADS), 0, st>>>(a);
-  }
+  QuantiseArgs a = {x, rows, cols, static_cast<uint8_t*>(q), reinterpret_cast<uint32_t*>(scale), (int)groups};
+  const int64_t per = (QUANT_THREADS / 64) * QUANT_ROWS, blocks = block_rows == 1 ? (rows * groups + per - 1) / per : scale_rows * groups * 4;
+  if (blocks >= (int64_t)1 << 24) return fail(LLAMARL_ERR_UNSUPPORTED, "matrix too large");
+  const auto kernel = block_rows == 1 ? (dt == LLAMARL_BF16 ? k_quantise_rows<uint16_t> : k_quantise_rows<float>)
+                                      : (dt == LLAMARL_BF16 ? k_quantise_tiles<uint16_t> : k_quantise_tiles<float>);
+  kernel<<<dim3((unsigned)blocks), dim3(QUANT_THREADS), 0, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
@@ -215,12 +212,8 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
     s = (tile == BLOCK_256 ? launch_block_partials<Blocks256> : launch_block_partials<Blocks128>)(a, x, st);
   }
   if (s != LLAMARL_OK) return s;
-  if (tile > BLOCK_FEW) {
-    constexpr int TOKENS = TARGET_THREADS / 64;
-    k_target_logits<<<dim3((unsigned)((N + TOKENS - 1) / TOKENS)), dim3(TARGET_THREADS), 0, st>>>(a, x);
-    HIP_TRY(hipGetLastError());
-  }
-  return launch_merge(a, logp, lse, nullptr, 0, st);
+  if (tile <= BLOCK_FEW) return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);
+  return launch_merge(a, logp, lse, nullptr, 0, BlockTarget{x, N, V, (int)d}, st);
 }
 
 }  // extern "C"

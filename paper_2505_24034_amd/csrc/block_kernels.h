@@ -45,32 +45,74 @@ __device__ __forceinline__ float magnitude8(const float (&x)[OPT_ITEMS]) {
 struct QuantiseArgs {
   const void* x;
   int64_t rows, cols;      // dense; cols a multiple of 16
-  int bf16;
   uint8_t* q;
   uint32_t* words;
   int groups;              // of 512 columns
 };
-// A wavefront takes 512 columns of a row: a block is 16 lanes of eight entries, the wavefront's four exponents are a word.
-constexpr int QUANT_THREADS = 256;
+// eight entries as they lie in memory
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<uint16_t> {
+  i32x4_t w;
+  __device__ __forceinline__ void load(const uint16_t* p) { w = *reinterpret_cast<const i32x4_t*>(p); }
+  __device__ __forceinline__ void clear() { w = i32x4_t{0, 0, 0, 0}; }
+  __device__ __forceinline__ void get(float (&o)[OPT_ITEMS]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = __uint_as_float((uint32_t)w[i] << 16);
+      o[2 * i + 1] = __uint_as_float((uint32_t)w[i] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Raw8<float> {
+  f32x4_t a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4_t*>(p);
+    b = *reinterpret_cast<const f32x4_t*>(p + 4);
+  }
+  __device__ __forceinline__ void clear() { a = b = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ void get(float (&o)[OPT_ITEMS]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[i] = a[i];
+      o[i + 4] = b[i];
+    }
+  }
+};
+// A wavefront takes 512 columns of a row, QUANT_ROWS of those at a time: a block is 16 lanes of eight entries, the wavefront's four
+// exponents are a word.
+constexpr int QUANT_THREADS = 256, QUANT_ROWS = 4;
+template <typename T>
 __global__ __launch_bounds__(QUANT_THREADS) void k_quantise_rows(QuantiseArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t units = a.rows * a.groups, stride = (int64_t)gridDim.x * (QUANT_THREADS / 64);
-  for (int64_t u = (int64_t)blockIdx.x * (QUANT_THREADS / 64) + wave_id(); u < units; u += stride) {
-    const int64_t row = u / a.groups;
-    const int group = (int)(u - row * a.groups);
-    const int64_t col = (int64_t)group * SCALE_GROUP + lane * OPT_ITEMS;
-    const int left = (int)max((int64_t)0, min(a.cols - col, (int64_t)OPT_ITEMS));      // eight or none
+  const int64_t units = a.rows * a.groups, first = ((int64_t)blockIdx.x * (QUANT_THREADS / 64) + wave_id()) * QUANT_ROWS;
+  Raw8<T> raw[QUANT_ROWS];
+  int64_t at[QUANT_ROWS];                            // first entry of the lane; negative: none
+#pragma unroll
+  for (int i = 0; i < QUANT_ROWS; ++i) {
+    const int64_t u = first + i, row = u / a.groups, col = (u - row * a.groups) * SCALE_GROUP + lane * OPT_ITEMS;
+    at[i] = u < units && col < a.cols ? row * a.cols + col : -1;
+    if (at[i] >= 0) raw[i].load(static_cast<const T*>(a.x) + at[i]);
+    else raw[i].clear();
+  }
+#pragma unroll
+  for (int i = 0; i < QUANT_ROWS; ++i) {
+    const int64_t u = first + i, row = u / a.groups;
+    if (u >= units) break;                           // wave-uniform
     float x[OPT_ITEMS];
-    load8(a.x, a.bf16 != 0, row * a.cols + col, left, true, x);
+    raw[i].get(x);
     const int e = block_exponent(row_max(magnitude8(x)));
-    if (left > 0) *reinterpret_cast<u32x2*>(a.q + row * a.cols + col) = quantise8(x, e);
+    if (at[i] >= 0) *reinterpret_cast<u32x2*>(a.q + at[i]) = quantise8(x, e);
     const uint32_t b = (uint32_t)(e + 127);
     const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)b, 0) | (uint32_t)__builtin_amdgcn_readlane((int)b, 16) << 8 |
                           (uint32_t)__builtin_amdgcn_readlane((int)b, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)b, 48) << 24;
-    if (lane == 0) a.words[(int64_t)group * a.rows + row] = word;
+    if (lane == 0) a.words[(u - row * a.groups) * a.rows + row] = word;
   }
 }
-// A workgroup takes one 128 x 128 block: 16 rows at a time, kept in registers until the block's maximum is known.
+// A workgroup takes one 128 x 128 block: 16 rows at a time, kept in registers, as they came, until the block's maximum is known.
+template <typename T>
 __global__ __launch_bounds__(QUANT_THREADS) void k_quantise_tiles(QuantiseArgs a) {
   constexpr int PASSES = SCALE_BLOCK / 16;
   const int64_t tile_rows = (a.rows + SCALE_BLOCK - 1) / SCALE_BLOCK;
@@ -78,14 +120,19 @@ __global__ __launch_bounds__(QUANT_THREADS) void k_quantise_tiles(QuantiseArgs a
   const int64_t tr = blockIdx.x / blocks;
   const int cb = (int)(blockIdx.x - tr * blocks);
   const int64_t row0 = tr * SCALE_BLOCK + threadIdx.x / 16, col = (int64_t)cb * SCALE_BLOCK + (threadIdx.x & 15) * OPT_ITEMS;
-  float x[PASSES][OPT_ITEMS], top = 0.f;
+  Raw8<T> raw[PASSES];
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
-    const bool there = row0 + 16 * p < a.rows && col < a.cols;
-    load8(a.x, a.bf16 != 0, (row0 + 16 * p) * a.cols + col, there ? OPT_ITEMS : 0, true, x[p]);
+    if (row0 + 16 * p < a.rows && col < a.cols) raw[p].load(static_cast<const T*>(a.x) + (row0 + 16 * p) * a.cols + col);
+    else raw[p].clear();
   }
+  float top = 0.f;
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p) top = fmaxf(top, magnitude8(x[p]));
+  for (int p = 0; p < PASSES; ++p) {
+    float x[OPT_ITEMS];
+    raw[p].get(x);
+    top = fmaxf(top, magnitude8(x));
+  }
   top = row_max(top);
   __shared__ float s_top[QUANT_THREADS / 16];
   if ((threadIdx.x & 15) == 0) s_top[threadIdx.x / 16] = top;
@@ -94,8 +141,11 @@ __global__ __launch_bounds__(QUANT_THREADS) void k_quantise_tiles(QuantiseArgs a
   for (int i = 0; i < QUANT_THREADS / 16; ++i) top = fmaxf(top, s_top[i]);
   const int e = block_exponent(top);
 #pragma unroll
-  for (int p = 0; p < PASSES; ++p)
-    if (row0 + 16 * p < a.rows && col < a.cols) *reinterpret_cast<u32x2*>(a.q + (row0 + 16 * p) * a.cols + col) = quantise8(x[p], e);
+  for (int p = 0; p < PASSES; ++p) {
+    float x[OPT_ITEMS];
+    raw[p].get(x);
+    if (row0 + 16 * p < a.rows && col < a.cols) *reinterpret_cast<u32x2*>(a.q + (row0 + 16 * p) * a.cols + col) = quantise8(x, e);
+  }
   if (threadIdx.x == 0) reinterpret_cast<uint8_t*>(a.words + (int64_t)(cb >> 2) * tile_rows + tr)[cb & 3] = (uint8_t)(e + 127);
 }
 
@@ -125,10 +175,10 @@ struct BlockLogitsArgs {
   int tiles_v, tiles_t;
   void* z;                 // [N][V]
 };
-// A tile's accumulators to z (its first logit): four neighbouring logits of a token a store.  fp32: buffer stores, whose lanes past
+// A tile's accumulators to z (its first logit), after(j) behind column block j: four neighbouring logits of a token a store.  fp32: buffer stores, whose lanes past
 // the matrix are put out of bounds: one offset a column is all that they keep in registers.
-template <typename S>
-__device__ __forceinline__ void store_tile(float* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT) {
+template <typename S, typename F>
+__device__ __forceinline__ void store_tile(float* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT, F after) {
   const uint64_t p = reinterpret_cast<uint64_t>(z);
   const auto rs = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p) |
                                                                            (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) << 32),
@@ -148,28 +198,34 @@ __device__ __forceinline__ void store_tile(float* z, int64_t V, const f32x4_t (&
           __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[i][j][r]), rs, (int)(lp.row(i, r) < rowsV ? at : OOB_OFFSET), 64 * i + 4 * r, 0);
     }
     LLAMARL_FENCE();
+    after(j);
+    LLAMARL_FENCE();
   }
 }
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));      // rows of z start wherever V puts them
-template <typename S>
-__device__ __forceinline__ void store_tile(uint16_t* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT) {
+template <typename S, typename F>
+__device__ __forceinline__ void store_tile(uint16_t* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT, F after) {
 #pragma unroll
   for (int j = 0; j < S::NB; ++j) {
-    if (lp.col(j) >= rowsT) continue;
-    uint16_t* at = z + lp.col(j) * V + lp.row(0, 0);
+    if (lp.col(j) < rowsT) {
+      uint16_t* at = z + lp.col(j) * V + lp.row(0, 0);
 #pragma unroll
-    for (int i = 0; i < S::MB; ++i) {
-      uint16_t b[4];
+      for (int i = 0; i < S::MB; ++i) {
+        uint16_t b[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) b[r] = float_to_bf16_bits(acc[i][j][r]);
-      if (lp.row(i, 3) < rowsV) {
-        *reinterpret_cast<u32x2_any*>(at + 16 * i) = u32x2_any{(uint32_t)b[0] | (uint32_t)b[1] << 16, (uint32_t)b[2] | (uint32_t)b[3] << 16};
-      } else {
+        for (int r = 0; r < 4; ++r) b[r] = float_to_bf16_bits(acc[i][j][r]);
+        if (lp.row(i, 3) < rowsV) {
+          *reinterpret_cast<u32x2_any*>(at + 16 * i) = u32x2_any{(uint32_t)b[0] | (uint32_t)b[1] << 16, (uint32_t)b[2] | (uint32_t)b[3] << 16};
+        } else {
 #pragma unroll
-        for (int r = 0; r < 3; ++r)
-          if (lp.row(i, r) < rowsV) at[16 * i + r] = b[r];
+          for (int r = 0; r < 3; ++r)
+            if (lp.row(i, r) < rowsV) at[16 * i + r] = b[r];
+        }
       }
     }
+    LLAMARL_FENCE();
+    after(j);
+    LLAMARL_FENCE();
   }
 }
 template <typename G, typename Out>
@@ -220,11 +276,13 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_block_logit
     if (!last) {
       cur.take(sch);
       setup(cur);
-#pragma unroll
-      for (int q = 0; q < G::FIRST_PARTS; ++q) g.issue_first(smem, q);
+      g.issue_first(smem, 0);
+      g.issue_first(smem, 1);
     }
     LLAMARL_FENCE();
-    store_tile<S>(static_cast<Out*>(a.z) + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT);
+    store_tile<S>(static_cast<Out*>(a.z) + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT, [&](int j) {
+      if (!last && j < 2) g.issue_first(smem, 2 + j);
+    });
     if (last) break;
   }
 }
@@ -239,30 +297,33 @@ __device__ __forceinline__ float e4m3_dot(uint32_t x, uint32_t y, float s) {
   return fmaf(c[1], e[1], fmaf(c[0], e[0], fmaf(a[1], b[1], fmaf(a[0], b[0], s))));
 }
 __device__ __forceinline__ int exponent_of(uint32_t word, int block) { return (int)(word >> 8 * (block & 3) & 0xffu) - 127; }
-constexpr int TARGET_THREADS = 256;
-__global__ __launch_bounds__(TARGET_THREADS) void k_target_logits(FwdArgs a, BlockHead x) {
-  const int64_t p = (int64_t)blockIdx.x * (TARGET_THREADS / 64) + wave_id();
-  if (p >= *a.n_act) return;
-  const int row = a.rows[p], y = a.targets[row], lane = threadIdx.x & 63;
-  const uint8_t *h = x.H + (int64_t)row * a.d, *w = x.W + (int64_t)y * a.d;
-  const int64_t w_rows = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK;
-  float z = 0.f;
-  for (int k = lane * 16; k < (int)a.d; k += 64 * 16) {
-    const i32x4_t u = *reinterpret_cast<const i32x4_t*>(h + k), v = *reinterpret_cast<const i32x4_t*>(w + k);
-    const int group = k / SCALE_GROUP, block = k / SCALE_BLOCK;
-    float s = 0.f;
+struct BlockTarget {       // for k_merge_logp
+  static constexpr bool FORMED = true;
+  BlockHead x;
+  int64_t N, V;
+  int d;
+  // of token `row` and vocabulary row y, in every lane of a wavefront
+  __device__ __forceinline__ float logit(int row, int y) const {
+    const int lane = threadIdx.x & 63;
+    const uint8_t *h = x.H + (int64_t)row * d, *w = x.W + (int64_t)y * d;
+    const int64_t w_rows = (V + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    float z = 0.f;
+    for (int k = lane * 16; k < d; k += 64 * 16) {
+      const i32x4_t u = *reinterpret_cast<const i32x4_t*>(h + k), v = *reinterpret_cast<const i32x4_t*>(w + k);
+      const int group = k / SCALE_GROUP, block = k / SCALE_BLOCK;
+      float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s = e4m3_dot((uint32_t)u[i], (uint32_t)v[i], s);
-    z += ldexpf(s, exponent_of(x.h_words[(int64_t)group * a.N + row], block) + exponent_of(x.w_words[(int64_t)group * w_rows + y / SCALE_BLOCK], block));
+      for (int i = 0; i < 4; ++i) s = e4m3_dot((uint32_t)u[i], (uint32_t)v[i], s);
+      z += ldexpf(s, exponent_of(x.h_words[(int64_t)group * N + row], block) + exponent_of(x.w_words[(int64_t)group * w_rows + y / SCALE_BLOCK], block));
+    }
+    return wave_sum(z);
   }
-  z = wave_sum(z);
-  if (lane == 0) a.zt[p] = z;
-}
+};
 
 // ---- few tokens ---------------------------------------------------------------------------------------------------------------------
 // Every byte of W is used for a few products only, and the time is W's way from memory: W goes from there to the registers of the
 // one wavefront that multiplies it.  The matrix pipe has time to spare, so the entries are widened to bf16, exactly, and multiplied
-// there: full fp32 sums (see k_target_logits), the scales on a block's sum.
+// there: full fp32 sums (see BlockTarget), the scales on a block's sum.
 struct FewArgs {
   BlockHead x;
   int64_t N, d, V;

@@ -77,6 +77,8 @@ struct BlockStreams {
   static constexpr int LDS_BYTES = 2 * STAGE;
   static constexpr int GROUPS_PER_CU = Shape::BM == 256 ? 1 : 2;
   static constexpr int FIRST_PARTS = 4;
+  static constexpr int YOUNGER = MB * NB + LoaderA::ITERS + LoaderB::ITERS + 2;      // see TileGemmBlocks::run
+  static_assert(YOUNGER < 64, "vmcnt counts to 63");
   static_assert(Shape::WAVE_M <= SCALE_BLOCK && NB == 4 && (MB == 8 || MB == 4), "a wavefront's rows share their scales; slot tables");
   LoaderA la;
   LoaderB lb;
@@ -256,12 +258,12 @@ struct TileGemmBlocks : BlockStreams<S_, Order_> {
     }
     if (BAR) sc.row = row_next;
   }
-  // counted (wave-uniform): MB * NB stores of the previous tile, and no other vector-memory operation, were issued after the first
-  // slabs were requested.  They drain under the first slab.
+  // counted (wave-uniform): the requests of the first slab were followed by those of the second and by MB * NB stores of the
+  // previous tile, and by no other vector-memory operation: the first slab alone is waited for.
   __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {
     const int nk = this->slabs();
     const Addresses ad = Base::addresses();
-    if (counted) wait_vmcnt<MB * NB>();
+    if (counted) wait_vmcnt<Base::YOUNGER>();
     else wait_vmcnt0();
     __syncthreads();
     frag_t a[4], b[NB];
@@ -360,7 +362,7 @@ struct TileGemmBlocksExact : BlockStreams<S_, Order_> {
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    if (counted) wait_vmcnt<MB * NB>();
+    if (counted) wait_vmcnt<Base::YOUNGER>();
     else wait_vmcnt0();
     __syncthreads();
     char *s = smem, *o = smem + Base::STAGE;

@@ -475,11 +475,15 @@ struct MergeArgs {
 };
 // PARTIAL: W is a shard of a vocabulary-parallel head; the per-token (m, s, zt) are what the shards would
 // all-reduce (paper Sec. 8.2, Table 3: trainer model parallelism 8-32), see k_merge_shards.
-template <bool PARTIAL, int TOKENS>
-__global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a) {
+// Target: forms the target logits of the block's tokens again (block_kernels.h), in place of zt.
+struct StoredTarget {
+  static constexpr bool FORMED = false;
+};
+template <bool PARTIAL, int TOKENS, typename Target>
+__global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a, Target target) {
   constexpr int SLICES = MERGE_THREADS / TOKENS, WAVES = MERGE_THREADS / 64;
   static_assert(TOKENS == 32 || TOKENS == 8, "cross-lane steps written for these");
-  __shared__ float s_M[WAVES][TOKENS], s_S[WAVES][TOKENS];
+  __shared__ float s_M[WAVES][TOKENS], s_S[WAVES][TOKENS], s_z[Target::FORMED ? TOKENS : 1];
   const int tok = threadIdx.x % TOKENS, sl = threadIdx.x / TOKENS;
   const int64_t p = (int64_t)blockIdx.x * TOKENS + tok;
   const int64_t n = *a.n_act;
@@ -529,6 +533,13 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a) {
     const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(S), __float_as_uint(S), false, false);
     merge(__uint_as_float(up ? m[0] : m[1]), __uint_as_float(up ? t[0] : t[1]));
   }
+  if constexpr (Target::FORMED) {
+    for (int q = wave_id(); q < TOKENS && (int64_t)blockIdx.x * TOKENS + q < n; q += WAVES) {      // wave-uniform
+      const int row = a.rows[(int64_t)blockIdx.x * TOKENS + q];
+      const float z = target.logit(row, a.targets[row]);
+      if ((threadIdx.x & 63) == 0) s_z[q] = z;
+    }
+  }
   if ((threadIdx.x & 63) < TOKENS) {
     s_M[threadIdx.x >> 6][tok] = M;
     s_S[threadIdx.x >> 6][tok] = S;
@@ -551,7 +562,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a) {
       // in double: lse and logp each carry one fp32 rounding, at the size of the result
       const double l = (double)Mx + log((double)Sx);
       a.out1[t] = (float)l;
-      a.out0[t] = (float)((double)a.zt[p] - l);
+      a.out0[t] = (float)((double)(Target::FORMED ? s_z[tok] : a.zt[p]) - l);
     }
   }
 }

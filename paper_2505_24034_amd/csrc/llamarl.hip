@@ -339,16 +339,18 @@ llamarl_status launch_bwd_dz(DzArgs a, int64_t rows, hipStream_t st) {
 }
 
 // the partials of a forward's tiles to its outputs, see run_logprobs
-llamarl_status launch_merge(const FwdArgs& a, float* out0, float* out1, float* out2, int partial, hipStream_t st) {
+template <typename Target>
+llamarl_status launch_merge(const FwdArgs& a, float* out0, float* out1, float* out2, int partial, const Target& target, hipStream_t st) {
   MergeArgs m;
   m.part_m = a.part_m; m.part_s = a.part_s; m.zt = a.zt; m.rows = a.rows; m.n_act = a.n_act; m.tiles_v = a.tiles_v;
   m.n_pad = a.n_pad; m.out0 = out0; m.out1 = out1; m.out2 = out2; m.targets = a.targets; m.v_off = a.v_off; m.V = a.V;
   // the log-prob call with d = 8 at (N, V), 8 / 32 tokens a block: (300, 128256) 24.2 / 26.0 us, (1041, 5003) 14.4 / 15.8,
   // (4097, 32000) 42.7 / 42.8, (8192, 60000) 109 / 103
   const int tokens = a.N <= 2048 ? 8 : 32;
-  const auto merge = tokens == 8 ? (partial ? k_merge_logp<true, 8> : k_merge_logp<false, 8>)
-                                 : (partial ? k_merge_logp<true, 32> : k_merge_logp<false, 32>);
-  merge<<<dim3((unsigned)((a.N + tokens - 1) / tokens)), dim3(MERGE_THREADS), 0, st>>>(m);
+  auto merge = tokens == 8 ? k_merge_logp<false, 8, Target> : k_merge_logp<false, 32, Target>;
+  if constexpr (!Target::FORMED)
+    if (partial) merge = tokens == 8 ? k_merge_logp<true, 8, Target> : k_merge_logp<true, 32, Target>;
+  merge<<<dim3((unsigned)((a.N + tokens - 1) / tokens)), dim3(MERGE_THREADS), 0, st>>>(m, target);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
@@ -384,7 +386,7 @@ llamarl_status run_logprobs(const void* H, const void* W, const int32_t* targets
   else
     s = (tile == TILE_128 ? launch_fwd_partials<F32Loop128> : launch_fwd_partials<F32Loop64>)(a, st);
   if (s != LLAMARL_OK) return s;
-  return launch_merge(a, out0, out1, out2, partial, st);
+  return launch_merge(a, out0, out1, out2, partial, StoredTarget(), st);
 }
 
 // active rows of each pass: cnt[c] = clamp(n_act - c * R, 0, R)

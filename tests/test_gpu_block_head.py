@@ -77,8 +77,8 @@ def _head(N, d, V, seed, spread=0.0):
 
 
 def _plain(x):
-    H, W = dequantise(x[0], x[1], 1), dequantise(x[2], x[3], 128)
-    return H @ W.T, np.sqrt((H * H) @ (W * W).T)
+    H, W = (torch.from_numpy(dequantise(q, s, b)).cuda() for q, s, b in ((x[0], x[1], 1), (x[2], x[3], 128)))
+    return (H @ W.T).cpu().numpy(), torch.sqrt((H * H) @ (W * W).T).cpu().numpy()      # products in 64 bits
 
 
 def _tolerance(z, rss, d, fp32, out_u):
