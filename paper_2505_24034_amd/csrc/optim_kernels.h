@@ -25,7 +25,8 @@
 namespace llamarl {
 
 constexpr int OPT_TENSORS = 48;              // tensors of a launch: 3.5 of the 4 KB of kernel arguments
-constexpr int OPT_THREADS = 256, OPT_ITEMS = 8, OPT_UNIT = OPT_THREADS * OPT_ITEMS;
+// 512 threads against 256: 8-bit states of the 8B head 1.57 -> 1.48 ms (mean of five runs each), 32-bit ones the same
+constexpr int OPT_THREADS = 512, OPT_ITEMS = 8, OPT_UNIT = OPT_THREADS * OPT_ITEMS;
 constexpr int STATE_BLOCK = 128;             // 16 lanes of eight entries: one row of a wavefront's cross-lane moves
 constexpr float E4M3_MAX = 448.f;
 constexpr float STATE_TINY = 0x1p-100f;      // a block whose largest magnitude is below this is held as zeros (its inverse overflows)
@@ -48,17 +49,16 @@ struct OptList {
   OptTensor t[OPT_TENSORS];
   int first[OPT_TENSORS + 1];                // first workgroup of each tensor
   int count;
-  int units;                                 // OPT_UNIT entries a workgroup takes
+  int units;                                 // of OPT_UNIT entries that a workgroup takes (k_adamw: one)
 };
-// tensor of this workgroup (uniform)
+// Tensor of this workgroup: the last whose first workgroup is not past it.  A lane looks at a tensor: one load, where a search would
+// be a chain of them, which a list of small tensors waits for.
+static_assert(OPT_TENSORS <= 64, "a lane a tensor");
 __device__ __forceinline__ int opt_tensor_of(const OptList& l) {
-  int at = 0;
-#pragma unroll
-  for (int step = 32; step > 0; step >>= 1)
-    if (at + step < l.count && l.first[at + step] <= (int)blockIdx.x) at += step;
-  return at;
+  const int lane = threadIdx.x & 63;
+  const uint64_t past = __ballot(lane < l.count && l.first[lane < OPT_TENSORS ? lane : 0] <= (int)blockIdx.x);
+  return 63 - __builtin_clzll(past);
 }
-static_assert(OPT_TENSORS <= 64, "six steps of the search");
 
 // Eight neighbouring entries from `at` on: 16-byte accesses where all eight exist and the tensor is aligned.
 __device__ __forceinline__ void load8(const float* x, int64_t at, int left, bool wide, float (&o)[OPT_ITEMS]) {
@@ -137,7 +137,12 @@ __global__ __launch_bounds__(OPT_THREADS) void k_grad_squares(OptList l, double*
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.x] = (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
+  if (threadIdx.x == 0) {
+    s = s_w[0];
+#pragma unroll
+    for (int w = 1; w < OPT_THREADS / 64; ++w) s += s_w[w];
+    part[blockIdx.x] = s;
+  }
 }
 // One workgroup; the sums in the order of the list.
 constexpr int NORM_THREADS = 1024;
@@ -175,12 +180,26 @@ __device__ __forceinline__ double power(double b, int64_t t) {
     if (t & 1) r *= b;
   return r;
 }
-// 1 ulp; v_sqrt_f32 alone loses what lies below the normal numbers
+// Rounded correctly: the estimate of 1 / sqrt(v), one step of Newton's iteration whose residual is exact.  v_rsq_f32 alone loses what
+// lies below the normal numbers.
 __device__ __forceinline__ float root(float v) {
   const bool small = v < 0x1p-96f;
-  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
-  return small ? r * 0x1p-32f : r;
+  const float x = small ? v * 0x1p64f : v, e = __builtin_amdgcn_rsqf(x);
+  const float s = x * e, r = fmaf(fmaf(-s, s, x), 0.5f * e, s);
+  return !(x > 0.f && x < INFINITY) ? x : small ? r * 0x1p-32f : r;
 }
+// x / s for several x, rounded correctly: the reciprocal is made once, and a quotient's residual is exact
+struct Quotient {
+  float s, inv;
+  __device__ __forceinline__ explicit Quotient(float s_) : s(s_) {
+    const float e = __builtin_amdgcn_rcpf(s_);
+    inv = fmaf(fmaf(-s_, e, 1.f), e, e);
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    const float q = x * inv;
+    return fmaf(fmaf(-q, s, x), inv, q);
+  }
+};
 // over the 16 lanes of a block's row, in every lane; a NaN is passed over
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __uint_as_float(dpp_move<ROW_ROR(8)>(__float_as_uint(x))));
@@ -238,11 +257,7 @@ __device__ __forceinline__ void store_states(uint8_t* q, int64_t at, int left, b
 }
 
 __global__ __launch_bounds__(OPT_THREADS) void k_adamw(AdamwArgs a) {
-  float gs = 1.f;
-  if (a.scale != nullptr) {
-    gs = *a.scale;
-    if (!(fabsf(gs) < INFINITY)) return;     // uniform: a step whose scale is not finite is not taken
-  }
+  const float gs = a.scale != nullptr ? *a.scale : 1.f;
   const float lr = a.lr_device != nullptr ? *a.lr_device : a.lr;
   float inv_c1 = a.inv_c1, inv_sqrt_c2 = a.inv_sqrt_c2;
   int64_t step = a.step;
@@ -253,78 +268,85 @@ __global__ __launch_bounds__(OPT_THREADS) void k_adamw(AdamwArgs a) {
   }
   const int ti = opt_tensor_of(a.l);
   const OptTensor& t = a.l.t[ti];
-  const int64_t n = t.n, from = (int64_t)((int)blockIdx.x - a.l.first[ti]) * a.l.units * OPT_UNIT;
+  const int64_t at = (int64_t)((int)blockIdx.x - a.l.first[ti]) * OPT_UNIT + threadIdx.x * OPT_ITEMS;
+  // lanes past the end stay: a block's row finds its maximum together
+  const int left = (int)max((int64_t)0, min(t.n - at, (int64_t)OPT_ITEMS));
   const int flags = t.flags;
   const bool wide = (flags & OPT_WIDE) != 0, p_bf16 = (flags & OPT_P_BF16) != 0, g_bf16 = (flags & OPT_G_BF16) != 0;
   const bool bits8 = (flags & OPT_8BIT) != 0;
-  for (int u = 0; u < a.l.units; ++u) {
-    const int64_t at = from + (int64_t)u * OPT_UNIT + threadIdx.x * OPT_ITEMS;
-    if (from + (int64_t)u * OPT_UNIT >= n) break;                  // uniform: all lanes of a block's row stay for its maximum
-    const int left = (int)max((int64_t)0, min(n - at, (int64_t)OPT_ITEMS));
-    float g[OPT_ITEMS], p[OPT_ITEMS], m[OPT_ITEMS], r[OPT_ITEMS];  // r: sqrt(v)
-    load8(t.g, g_bf16, at, left, wide, g);
-    if (t.master != nullptr) load8(t.master, at, left, wide, p);
-    else load8(t.p, p_bf16, at, left, wide, p);
-    if (!bits8) {
-      float v[OPT_ITEMS];
-      load8(static_cast<const float*>(t.m), at, left, wide, m);
-      load8(static_cast<const float*>(t.v), at, left, wide, v);
+  float g[OPT_ITEMS], p[OPT_ITEMS], m[OPT_ITEMS], r[OPT_ITEMS];  // r: sqrt(v)
+  load8(t.g, g_bf16, at, left, wide, g);
+  // A step whose scale is not finite is not taken.  Asked here, not before the loads: the scale is a load itself.
+  const bool taken = fabsf(gs) < INFINITY; // uniform
+  if (t.master != nullptr) load8(t.master, at, left, wide, p);
+  else load8(t.p, p_bf16, at, left, wide, p);
+  if (!bits8) {
+    float v[OPT_ITEMS];
+    load8(static_cast<const float*>(t.m), at, left, wide, m);
+    load8(static_cast<const float*>(t.v), at, left, wide, v);
+    if (!taken) return;
+#pragma unroll
+    for (int i = 0; i < OPT_ITEMS; ++i) {
+      const float x = g[i] * gs;
+      m[i] = fmaf(a.b1, m[i], a.one_b1 * x);
+      v[i] = fmaf(a.b2, v[i], a.one_b2 * x * x);
+      r[i] = root(v[i]);
+    }
+    store8(static_cast<float*>(t.m), at, left, wide, m);
+    store8(static_cast<float*>(t.v), at, left, wide, v);
+  } else {
+    const int64_t block = at / STATE_BLOCK;
+    float ms = 0.f, rs = 0.f;
+    if (left > 0) {
+      ms = t.m_scale[block];
+      rs = t.v_scale[block];
+    }
+    load_states(static_cast<const uint8_t*>(t.m), ms, at, left, wide, m);
+    load_states(static_cast<const uint8_t*>(t.v), rs, at, left, wide, r);
+    if (!taken) return;
+    float top_m = 0.f, top_r = 0.f;
+    {
+      // Every operation rounded by itself, so that the codes are what the formula gives in any other program: a last bit can turn a code,
+      // a code turn the block's next largest magnitude, and two runs of a model then part.
+#pragma clang fp contract(off)
 #pragma unroll
       for (int i = 0; i < OPT_ITEMS; ++i) {
         const float x = g[i] * gs;
-        m[i] = fmaf(a.b1, m[i], a.one_b1 * x);
-        v[i] = fmaf(a.b2, v[i], a.one_b2 * x * x);
-        r[i] = root(v[i]);
-      }
-      store8(static_cast<float*>(t.m), at, left, wide, m);
-      store8(static_cast<float*>(t.v), at, left, wide, v);
-    } else {
-      const int64_t block = at / STATE_BLOCK;
-      float ms = 0.f, rs = 0.f;
-      if (left > 0) {
-        ms = t.m_scale[block];
-        rs = t.v_scale[block];
-      }
-      load_states(static_cast<const uint8_t*>(t.m), ms, at, left, wide, m);
-      load_states(static_cast<const uint8_t*>(t.v), rs, at, left, wide, r);
-      float top_m = 0.f, top_r = 0.f;
-#pragma unroll
-      for (int i = 0; i < OPT_ITEMS; ++i) {
-        const float x = g[i] * gs;
-        m[i] = fmaf(a.b1, m[i], a.one_b1 * x);
-        r[i] = root(fmaf(a.b2, r[i] * r[i], a.one_b2 * x * x));
+        m[i] = m[i] * a.b1 + x * a.one_b1;
+        r[i] = root(r[i] * r[i] * a.b2 + x * x * a.one_b2);
         top_m = fmaxf(top_m, fabsf(m[i]));
         top_r = fmaxf(top_r, r[i]);
       }
-      top_m = row_max(top_m);
-      top_r = row_max(top_r);
-      const float sm = top_m < STATE_TINY ? 0.f : top_m * (1.f / E4M3_MAX), sr = top_r < STATE_TINY ? 0.f : top_r * (1.f / E4M3_MAX);
-      const float im = sm > 0.f ? E4M3_MAX * __builtin_amdgcn_rcpf(top_m) : 0.f, ir = sr > 0.f ? E4M3_MAX * __builtin_amdgcn_rcpf(top_r) : 0.f;
-      u32x2 qm, qr;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int e = 4 * h;
-        qm[h] = to_e4m3(m[e] * im, m[e + 1] * im, m[e + 2] * im, m[e + 3] * im);
-        const uint32_t pair = (uint32_t)(at >> 1) + 2 * h;
-        const uint32_t x = rounding_bits(pair, (uint32_t)step, t.place), y = rounding_bits(pair + 1, (uint32_t)step, t.place);
-        qr[h] = to_e4m3(round_by(r[e] * ir, x & 0xffffu), round_by(r[e + 1] * ir, x >> 16), round_by(r[e + 2] * ir, y & 0xffffu),
-                        round_by(r[e + 3] * ir, y >> 16));
-      }
-      store_states(static_cast<uint8_t*>(t.m), at, left, wide, qm);
-      store_states(static_cast<uint8_t*>(t.v), at, left, wide, qr);
-      if (left > 0 && (threadIdx.x & 15) == 0) {
-        t.m_scale[block] = sm;
-        t.v_scale[block] = sr;
-      }
     }
-    // the change is summed before it is taken off: lr wd is below the last bit of 1 for the learning rates in use
+    top_m = row_max(top_m);
+    top_r = row_max(top_r);
+    const float sm = top_m < STATE_TINY ? 0.f : top_m * (1.f / E4M3_MAX), sr = top_r < STATE_TINY ? 0.f : top_r * (1.f / E4M3_MAX);
+    const Quotient by_m(sm > 0.f ? sm : 1.f), by_r(sr > 0.f ? sr : 1.f);
+    const float keep_m = sm > 0.f ? 1.f : 0.f, keep_r = sr > 0.f ? 1.f : 0.f;
+    u32x2 qm, qr;
 #pragma unroll
-    for (int i = 0; i < OPT_ITEMS; ++i)
-      p[i] -= lr * fmaf(a.decay, p[i], m[i] * inv_c1 * __builtin_amdgcn_rcpf(fmaf(r[i], inv_sqrt_c2, a.eps)));
-    if (t.master != nullptr) store8(t.master, at, left, wide, p);
-    if (p_bf16) store8(static_cast<uint16_t*>(t.p), at, left, wide, p);
-    else store8(static_cast<float*>(t.p), at, left, wide, p);
+    for (int h = 0; h < 2; ++h) {
+      const int e = 4 * h;
+      qm[h] = to_e4m3(by_m(m[e] * keep_m), by_m(m[e + 1] * keep_m), by_m(m[e + 2] * keep_m), by_m(m[e + 3] * keep_m));
+      const uint32_t pair = (uint32_t)(at >> 1) + 2 * h;
+      const uint32_t x = rounding_bits(pair, (uint32_t)step, t.place), y = rounding_bits(pair + 1, (uint32_t)step, t.place);
+      qr[h] = to_e4m3(round_by(by_r(r[e] * keep_r), x & 0xffffu), round_by(by_r(r[e + 1] * keep_r), x >> 16),
+                      round_by(by_r(r[e + 2] * keep_r), y & 0xffffu), round_by(by_r(r[e + 3] * keep_r), y >> 16));
+    }
+    store_states(static_cast<uint8_t*>(t.m), at, left, wide, qm);
+    store_states(static_cast<uint8_t*>(t.v), at, left, wide, qr);
+    if (left > 0 && (threadIdx.x & 15) == 0) {
+      t.m_scale[block] = sm;
+      t.v_scale[block] = sr;
+    }
   }
+  // the change is summed before it is taken off: lr wd is below the last bit of 1 for the learning rates in use
+#pragma unroll
+  for (int i = 0; i < OPT_ITEMS; ++i)
+    p[i] -= lr * fmaf(a.decay, p[i], m[i] * inv_c1 * __builtin_amdgcn_rcpf(fmaf(r[i], inv_sqrt_c2, a.eps)));
+  if (t.master != nullptr) store8(t.master, at, left, wide, p);
+  if (p_bf16) store8(static_cast<uint16_t*>(t.p), at, left, wide, p);
+  else store8(static_cast<float*>(t.p), at, left, wide, p);
 }
 
 }  // namespace llamarl
