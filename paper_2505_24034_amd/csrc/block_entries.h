@@ -6,53 +6,20 @@ namespace {
 
 typedef TileGemmBlocks<Shape256, SlabRing> Blocks256;
 typedef TileGemmBlocks<Shape128, SlabRing> Blocks128;
-typedef TileGemmBlocksExact<Shape128, SlabRing> BlocksExact;
+typedef TileGemmBlocksSimple<Shape64x64, SlabRing, false> Blocks64;
+typedef TileGemmBlocksSimple<Shape128, SlabRing, true> Exact128;
+typedef TileGemmBlocksSimple<Shape64x64, SlabRing, true> Exact64;
 
-// Which kernel a product of N tokens with V rows of W takes.  us at (N, V, d), weights that are in no cache:
-//                            fp32 logits: direct / through LDS / tiles       bf16 logits, log-probs on 128-tiles : through LDS
-//   (1, 128256, 4096)          97 / 103 / 99                                   93, 110 : 103
-//   (16, 128256, 4096)        153 / 114 / 103                                  96, 111 : 114
-//   (48, 128256, 4096)          - / 134 / 113                                 104, 116 : 133, 160
-//   (1, 16032, 8192)           29 / 29 / 83                                    58,  72 : 29
-//   (16, 16032, 8192)          41 / 30 / 84                                    59,  74 : 30
-//   (48, 16032, 8192)           - / 33 / 85                                    61,  75 : 33,  45
-//   (1, 33001, 2048)           15 / 20 / 24                                    16,  27 : 20
-//   (48, 33001, 2048)           - / 28 / 25                                    17,  29 : 28,  44
-//   (16, 5003, 1024)          6.2 / 6.2 / 13.6                                7.4,  18 : 6.2
-//   (8, 1000, 8192)           8.8 / 18.7 / 81                                  32,  50 : 19
-//   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
-// So tiles of 128 rows where there is one for every CU (fp32 ones: two), below that the direct kernel for up to four tokens and for few
-// rows, the one through LDS to 64 tokens.
-enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_128, BLOCK_256 };
-BlockTile block_tile(int64_t N, int64_t V, bool exact) {
-  if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
-  // 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, bf16 logits, us at (N, V, d): (128, 128256, 4096) 127 : 123,
-  // (256, ..) 153 : 194, (300, ..) 211 : 236, (1024, ..) 524 : 667, (1900, 33001, 2048) 160 : 161, (2048, 16032, 8192) 209 : 271, (700, 8000, 1024)
-  // 22 : 15, (1041, 5003, 528) 21 : 13
-  return N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
-}
-// wavefronts of k_few_direct that share rows of W: as many as have a group of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192) 51 / 32 / 32 / 29,
-// (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23
-int direct_parts(int64_t d) {
-  const int64_t groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
-  return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
-}
-// rows of W that a tile of partials has
-int block_tile_rows(BlockTile t, int64_t d) {
-  return t == BLOCK_256 ? 256 : t == BLOCK_128 ? 128 : t == BLOCK_FEW ? FEW_ROWS : std::min(FEW_WAVES / direct_parts(d) * 16, 64);
-}
-
-// As FwdWs.  The size must not fall as N or V grows: room for 128-row tiles of N tokens and for the many rows of partials of a
-// call of few.
+// As FwdWs; the planes: block_partials.
 struct BlockWs {
-  int64_t n_pad;
+  int64_t n_pad, plane;      // plane: floats
   size_t off_m, off_s, off_zt, off_rows, off_nact, total;
 };
 BlockWs block_ws(int64_t N, int64_t V) {
   BlockWs w;
   w.n_pad = round_up(N, 64);
-  const int64_t few = (V + 15) / 16 * 64, many = (V + 127) / 128 * w.n_pad;
-  const int64_t plane = round_up(std::max(few, many) * 4, 256), per_token = round_up(w.n_pad * 4, 256);
+  w.plane = block_partials(N, V);
+  const int64_t plane = round_up(w.plane * 4, 256), per_token = round_up(w.n_pad * 4, 256);
   w.off_m = 0;
   w.off_s = (size_t)plane;
   w.off_zt = w.off_s + (size_t)plane;
@@ -99,7 +66,7 @@ llamarl_status launch_few(FewArgs a, BlockTile tile, hipStream_t st) {
             : a.N <= 48 ? launch_few_blocks<3, Out>
                         : launch_few_blocks<4, Out>)(a, st);
   a.parts = direct_parts(a.d);
-  const int rows = FEW_WAVES / a.parts * 16;
+  const int rows = DIRECT_WAVES / a.parts * 16;
   k_few_direct<Out><<<dim3((unsigned)((a.V + rows - 1) / rows)), dim3(FEW_THREADS), 0, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
@@ -170,8 +137,10 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   }
   BlockLogitsArgs a = {};
   a.x = x; a.N = N; a.d = d; a.V = V; a.z = z;
-  if (z_dt == LLAMARL_F32) return launch_block_logits<BlocksExact, float>(a, st);
-  return tile == BLOCK_256 ? launch_block_logits<Blocks256, uint16_t>(a, st) : launch_block_logits<Blocks128, uint16_t>(a, st);
+  if (z_dt == LLAMARL_F32) return (tile == BLOCK_64 ? launch_block_logits<Exact64, float> : launch_block_logits<Exact128, float>)(a, st);
+  return (tile == BLOCK_256   ? launch_block_logits<Blocks256, uint16_t>
+          : tile == BLOCK_128 ? launch_block_logits<Blocks128, uint16_t>
+                              : launch_block_logits<Blocks64, uint16_t>)(a, st);
 }
 
 size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) { return N <= 0 || V <= 0 ? 0 : block_ws(N, V).total; }
@@ -197,6 +166,7 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
   a.H = H; a.W = W; a.targets = targets; a.N = N; a.d = d; a.V = V;
   a.tiles_v = (int)((V + tile_rows - 1) / tile_rows);
   a.n_pad = w.n_pad;
+  if (a.tiles_v * w.n_pad > w.plane) return fail(LLAMARL_ERR_WORKSPACE, "partials of %d tiles do not fit", a.tiles_v);      // a mistake in the rules
   a.part_m = reinterpret_cast<float*>(base + w.off_m);
   a.part_s = reinterpret_cast<float*>(base + w.off_s);
   a.zt = reinterpret_cast<float*>(base + w.off_zt);
@@ -209,7 +179,9 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
     f.x = x; f.N = N; f.d = d; f.V = V; f.f = a;
     s = launch_few<void>(f, tile, st);
   } else {
-    s = (tile == BLOCK_256 ? launch_block_partials<Blocks256> : launch_block_partials<Blocks128>)(a, x, st);
+    s = (tile == BLOCK_256   ? launch_block_partials<Blocks256>
+         : tile == BLOCK_128 ? launch_block_partials<Blocks128>
+                             : launch_block_partials<Blocks64>)(a, x, st);
   }
   if (s != LLAMARL_OK) return s;
   if (tile <= BLOCK_FEW) return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);

@@ -331,7 +331,7 @@ struct FewArgs {
   void* z;                 // logits: [N][V]
   FwdArgs f;               // log-probs: rows, n_act, targets, n_pad, part_m, part_s, zt;  tile: the rows of a workgroup
 };
-constexpr int FEW_WAVES = 8, FEW_THREADS = 64 * FEW_WAVES;
+constexpr int FEW_WAVES = DIRECT_WAVES, FEW_THREADS = 64 * FEW_WAVES;
 // z of up to 64 rows of W (a lane each) and a token: stored, or reduced to the tile's partials
 template <typename Out>
 __device__ __forceinline__ void few_result(const FewArgs& a, int pos, int64_t first, int rows, int64_t tile, float z) {
@@ -368,7 +368,6 @@ __device__ __forceinline__ int few_token(const FewArgs& a, int at, int n_act) { 
 }
 
 // Up to 16 tokens.  A wavefront takes 16 rows of W and every parts-th group of 512 columns, all of it from memory to registers.
-constexpr int DIRECT_TOKENS = 16;
 template <typename Out>
 __global__ __launch_bounds__(FEW_THREADS, 4) void k_few_direct(FewArgs a) {
   constexpr int PITCH = 16 + 4;                      // floats of a token's row in LDS
@@ -443,7 +442,6 @@ __global__ __launch_bounds__(FEW_THREADS, 4) void k_few_direct(FewArgs a) {
 // order.  The tokens' part of a group is brought to LDS once for the four wavefronts of a half: read by each of them from L2 it was more
 // traffic than W's (48 tokens 217 - 250 us of a 128256 x 4096 head, 134 here).  W's registers are loaded again, for the next group, as soon as a
 // block is multiplied.  Workgroups start at groups of their own: see SlabOrder.
-constexpr int FEW_TOKENS = 64, FEW_ROWS = 64;
 constexpr int FEW_PITCH = FEW_ROWS + 4;              // floats of a token's row in LDS
 template <int NB>
 constexpr int FEW_SLAB = NB * 16 * SLAB_ROW_BYTES;   // a block of 128 columns of the tokens

@@ -61,7 +61,8 @@ struct ScaleWords {
   }
 };
 
-// What the loops share: operand streams, scale words, stages.  Shape256: 256 x 256, one workgroup a CU.  Shape128: 128 x 128, two.
+typedef TileShape<2, 2, 2, 2> Shape64x64;     // 4 wavefronts of 32 x 32
+// What the loops share: operand streams, scale words, stages.  One workgroup of 256 x 256 tiles a CU, two of 128 x 128, four of 64 x 64.
 template <typename S_, typename Order_>
 struct BlockStreams {
   typedef FP8 Type;
@@ -75,11 +76,11 @@ struct BlockStreams {
   static constexpr int COL_WORDS = Shape::STAGE_BYTES, ROW_WORDS = COL_WORDS + Shape::BN * 4;      // in a stage
   static constexpr int STAGE = ROW_WORDS + Shape::WAVES * 256;
   static constexpr int LDS_BYTES = 2 * STAGE;
-  static constexpr int GROUPS_PER_CU = Shape::BM == 256 ? 1 : 2;
+  static constexpr int GROUPS_PER_CU = Shape::BM == 256 ? 1 : Shape::BM == 128 ? 2 : 4;
   static constexpr int FIRST_PARTS = 4;
   static constexpr int YOUNGER = MB * NB + LoaderA::ITERS + LoaderB::ITERS + 2;      // see TileGemmBlocks::run
   static_assert(YOUNGER < 64, "vmcnt counts to 63");
-  static_assert(Shape::WAVE_M <= SCALE_BLOCK && NB == 4 && (MB == 8 || MB == 4), "a wavefront's rows share their scales; slot tables");
+  static_assert(Shape::WAVE_M <= SCALE_BLOCK && Shape::BN % 64 == 0, "a wavefront's rows share their scales; words of 64 columns a request");
   LoaderA la;
   LoaderB lb;
   ScaleWords wa, wb;
@@ -212,7 +213,7 @@ struct TileGemmBlocks : BlockStreams<S_, Order_> {
                                        const Addresses& ad, int k_cur, int k_fetch) const {
     constexpr int PAIRS = MB / 2, LAST = 8 * (PAIRS - 1), TB = LAST - 5;
     constexpr int LA = Base::LoaderA::ITERS, LB = Base::LoaderB::ITERS;
-    static_assert(LA + LB == 8 && TB + 1 + load_slot(8) < 8 * PAIRS, "every load has a slot");
+    static_assert(NB == 4 && (MB == 8 || MB == 4) && LA + LB == 8 && TB + 1 + load_slot(8) < 8 * PAIRS, "every load has a slot");
     const int lane = threadIdx.x & 63, wave = wave_id();
     i32x4_t ra, rb;
     if (FETCH) {
@@ -305,11 +306,13 @@ __device__ __forceinline__ float scale_product(uint32_t a, uint32_t b) {
   return __builtin_amdgcn_ldexpf(1.f, min((int)(a & 0xffu) + (int)(b & 0xffu) - 254, 127));
 }
 
-// The same streams with fp32 sums: fragments are widened to bf16 and multiplied there, a block's sum is scaled into the accumulators.  128
-// widenings and 64 fused multiply-adds beside 64 MFMAs of 16 cycles a wavefront and slab: the vector instructions of one wavefront run
-// under the other's MFMAs.
-template <typename S_, typename Order_>
-struct TileGemmBlocksExact : BlockStreams<S_, Order_> {
+// Loops without an order of their own: a slab's fragments are read and multiplied as the compiler places them.
+//   EXACT   fp32 sums: fragments are widened to bf16 and multiplied there, a block's sum is scaled into the accumulators.  128 x 128: 128
+//           widenings and 64 fused multiply-adds beside 64 MFMAs of 16 cycles a wavefront and slab; 1000 tokens of a 128256 x 4096 head run
+//           at 0.97 PFLOP/s.  (The three interleaved by hand, one MFMA and two or three of the others: the same within 3 %.)
+//   else    on the 8-bit pipe; 64 x 64 tiles, where few larger ones would leave CUs without work
+template <typename S_, typename Order_, bool EXACT>
+struct TileGemmBlocksSimple : BlockStreams<S_, Order_> {
   typedef BlockStreams<S_, Order_> Base;
   typedef S_ Shape;
   typedef typename Base::Addresses Addresses;
@@ -318,41 +321,55 @@ struct TileGemmBlocksExact : BlockStreams<S_, Order_> {
   using Base::NB;
   using Base::slab_k;
   using Base::word;
-  static_assert(MB == 4, "sums of a slab beside the accumulators");
 
   __device__ __forceinline__ static void slab(const char* st, const Addresses& ad, f32x4_t (&acc)[MB][NB], int k0) {
-    f32x4_t sum[MB][NB];
+    const uint32_t row = Base::pick(word(st + ad.rw), k0);
+    uint32_t col[NB];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      i32x4_t x[MB], y[NB];
+    for (int j = 0; j < NB; ++j) col[j] = Base::pick(word(st + ad.cw + j * 64), k0);
+    if constexpr (!EXACT) {
+      i32x8_t b[NB];
 #pragma unroll
-      for (int j = 0; j < NB; ++j) y[j] = *reinterpret_cast<const i32x4_t*>(st + ad.b[c] + j * BLOCK_BYTES);
+      for (int j = 0; j < NB; ++j) b[j] = Base::frag_b(st, ad, j);
 #pragma unroll
-      for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const i32x4_t*>(st + ad.a[c] + i * BLOCK_BYTES);
+      for (int i = 0; i < MB; ++i) {
+        const i32x8_t a = Base::frag_a(st, ad, i);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {                  // 32 of a block's columns: eight entries a lane
-        bf16x8_t b[NB];
+        for (int j = 0; j < NB; ++j) mma_blocks(a, b[j], acc[i][j], (int)row, (int)col[j]);
+      }
+    } else {
+      f32x4_t sum[MB][NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) b[j] = widen(y[j][2 * h], y[j][2 * h + 1]);
+      for (int c = 0; c < 2; ++c) {
+        i32x4_t x[MB], y[NB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
-          const bf16x8_t a = widen(x[i][2 * h], x[i][2 * h + 1]);
+        for (int j = 0; j < NB; ++j) y[j] = *reinterpret_cast<const i32x4_t*>(st + ad.b[c] + j * BLOCK_BYTES);
 #pragma unroll
-          for (int j = 0; j < NB; ++j) {
-            if (c == 0 && h == 0) sum[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            mma(a, b[j], sum[i][j]);
+        for (int i = 0; i < MB; ++i) x[i] = *reinterpret_cast<const i32x4_t*>(st + ad.a[c] + i * BLOCK_BYTES);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                // 32 of a block's columns: eight entries a lane
+          bf16x8_t b[NB];
+#pragma unroll
+          for (int j = 0; j < NB; ++j) b[j] = widen(y[j][2 * h], y[j][2 * h + 1]);
+#pragma unroll
+          for (int i = 0; i < MB; ++i) {
+            const bf16x8_t a = widen(x[i][2 * h], x[i][2 * h + 1]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+              if (c == 0 && h == 0) sum[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+              mma(a, b[j], sum[i][j]);
+            }
           }
         }
       }
-    }
-    const uint32_t row = Base::pick(word(st + ad.rw), k0);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const float s = scale_product(row, Base::pick(word(st + ad.cw + j * 64), k0));
+      for (int j = 0; j < NB; ++j) {
+        const float s = scale_product(row, col[j]);
 #pragma unroll
-      for (int i = 0; i < MB; ++i)
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(sum[i][j][r], s, acc[i][j][r]);
+          for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(sum[i][j][r], s, acc[i][j][r]);
+      }
     }
   }
   __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {      // see TileGemmBlocks::run

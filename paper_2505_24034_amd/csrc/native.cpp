@@ -663,6 +663,13 @@ PyObject* logits_width(PyObject* const* a) {
   return PyLong_FromLong(rule((int)integer(a[0]), (int)integer(a[1]), integer(a[2]), (int)integer(a[3])).width);
 }
 
+// N, V, d, fp32 logits: kernel (BlockTile) of a product with an 8-bit head, rows of its tiles of partials, floats of their planes
+PyObject* block_plan(PyObject* const* a) {
+  const int64_t N = integer(a[0]), V = integer(a[1]);
+  const llamarl::BlockTile t = llamarl::block_tile(N, V, integer(a[3]) != 0);
+  return Py_BuildValue("iiL", (int)t, llamarl::block_tile_rows(t, integer(a[2])), (long long)llamarl::block_partials(N, V));
+}
+
 template <PyObject* (*F)(PyObject* const*), int NARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -690,7 +697,7 @@ PyMethodDef g_methods[] = {
     ENTRY(token_logprobs, 6), ENTRY(token_logprobs_partial, 8), ENTRY(merge_partials, 4), ENTRY(offpolicy_loss_fwd, 15),
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
     ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
-    ENTRY(token_logprobs_blocks, 8), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(token_logprobs_blocks, 8), ENTRY(block_plan, 4), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

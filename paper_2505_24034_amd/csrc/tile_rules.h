@@ -255,4 +255,55 @@ LLAMARL_RULE int pair_workgroups(int cus, int own, int other, bool own_long, boo
   return !own_long ? cus * own : cus * (other_long && other < own ? other : own) / 2;
 }
 
+// ---- heads in 8 bits (block_kernels.h) -----------------------------------------------------------------------------------
+constexpr int64_t DIRECT_TOKENS = 16, FEW_TOKENS = 64;        // most tokens of k_few_direct and k_few_tokens
+constexpr int DIRECT_WAVES = 8, FEW_ROWS = 64;
+// Which kernel a product of N tokens with V rows of W takes.  us at (N, V, d), weights that are in no cache:
+//                            fp32 logits: direct / through LDS / tiles       bf16 logits, log-probs on 128-tiles : through LDS
+//   (1, 128256, 4096)          97 / 103 / 99                                   93, 110 : 103
+//   (16, 128256, 4096)        153 / 114 / 103                                  96, 111 : 114
+//   (48, 128256, 4096)          - / 134 / 113                                 104, 116 : 133, 160
+//   (1, 16032, 8192)           29 / 29 / 83                                    58,  72 : 29
+//   (16, 16032, 8192)          41 / 30 / 84                                    59,  74 : 30
+//   (48, 16032, 8192)           - / 33 / 85                                    61,  75 : 33,  45
+//   (1, 33001, 2048)           15 / 20 / 24                                    16,  27 : 20
+//   (48, 33001, 2048)           - / 28 / 25                                    17,  29 : 28,  44
+//   (16, 5003, 1024)          6.2 / 6.2 / 13.6                                7.4,  18 : 6.2
+//   (8, 1000, 8192)           8.8 / 18.7 / 81                                  32,  50 : 19
+//   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
+// So tiles of 128 rows where there is one for every CU (fp32 ones: two), below that the direct kernel for up to four tokens and for few
+// rows, the one through LDS to 64 tokens.
+enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_64, BLOCK_128, BLOCK_256 };
+// Fewer tiles of 128 x 128 than this are cut into 64 x 64.  us at (N, V, d), 128 / 64, fp32 | bf16: (100, 4346, 1104) 18 / 9.0 | 9.9 / 6.5,
+// (200, 1000, 4096) 48 / 21 | 20 / 13, (100, 16032, 8192) 85 / 52 | 45 / 35, (300, 8000, 1024) 18.3 / 14.5 | 10.7 / 10.2 (log-probs 16.9 / 18.2),
+// (128, 33001, 4096) 67 / 53 | 36 / 39, (1041, 5003, 528) 18.6 / 22.3 | 13.4 / 19.1
+constexpr int64_t BLOCK_64_TILES = 128, EXACT_64_TILES = 288;
+LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
+  if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
+  if (tile_count(N, V, 128) < (exact ? EXACT_64_TILES : BLOCK_64_TILES)) return BLOCK_64;
+  // 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, bf16 logits, us at (N, V, d): (128, 128256, 4096) 127 : 123,
+  // (256, ..) 153 : 194, (300, ..) 211 : 236, (1024, ..) 524 : 667, (1900, 33001, 2048) 160 : 161, (2048, 16032, 8192) 209 : 271, (700, 8000, 1024)
+  // 22 : 15, (1041, 5003, 528) 21 : 13
+  return !exact && N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
+}
+// wavefronts of k_few_direct that share rows of W: as many as have a group (512 columns) of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192)
+// 51 / 32 / 32 / 29, (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23
+LLAMARL_RULE int direct_parts(int64_t d) {
+  const int64_t groups = (d + 511) / 512;
+  return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
+}
+// rows of W that a tile of partials has
+LLAMARL_RULE int block_tile_rows(BlockTile t, int64_t d) {
+  const int direct = DIRECT_WAVES / direct_parts(d) * 16;
+  return t == BLOCK_256 ? 256 : t == BLOCK_128 ? 128 : t == BLOCK_64 ? 64 : t == BLOCK_FEW ? FEW_ROWS : direct < 64 ? direct : 64;
+}
+// Floats of a plane of partials that serves any call of up to N tokens and V rows: 128-row tiles (or larger) of all tokens; 64-row
+// tiles, which are fewer than BLOCK_64_TILES of 128 x 128, each two rows of partials of 128 tokens; 16-row ones of up to 64 tokens.
+LLAMARL_RULE int64_t block_partials(int64_t N, int64_t V) {
+  const int64_t n_pad = (N + 63) / 64 * 64;
+  const int64_t large = (V + 127) / 128 * n_pad, small = (V + 63) / 64 * n_pad, few = (V + 15) / 16 * FEW_TOKENS;
+  const int64_t most = 256 * BLOCK_64_TILES, s = small < most ? small : most;
+  return large > few ? (large > s ? large : s) : few > s ? few : s;
+}
+
 }  // namespace llamarl

@@ -103,8 +103,9 @@ def test_logits(lib, i, N, dtype):
         assert torch.equal(got, lib.logits_blocks(*x, dtype=dtype))        # the same call gives the same bits
 
 
-@pytest.mark.parametrize("N,d,V,dtype", [(300, 1168, 50001, torch.bfloat16), (70, 2048, 60000, torch.bfloat16), (1100, 272, 12345, torch.bfloat16),
-                                         (64, 4624, 30000, torch.float32), (150, 656, 20011, torch.float32), (2000, 128, 8200, torch.bfloat16)])
+@pytest.mark.parametrize("N,d,V,dtype", [(300, 1168, 20001, torch.bfloat16), (70, 2048, 33000, torch.bfloat16), (1100, 272, 12345, torch.bfloat16),
+                                         (64, 4624, 10000, torch.float32), (150, 656, 20011, torch.float32), (2000, 128, 8200, torch.bfloat16),
+                                         (300, 1024, 8000, torch.float32), (300, 1024, 8000, torch.bfloat16), (3000, 144, 500, torch.bfloat16)])
 def test_logits_of_many_tiles(lib, N, d, V, dtype):
     """more tiles than workgroups, turned slabs (few columns of tiles), every kernel's last tile in both directions"""
     x = _head(N, d, V, N)
@@ -163,7 +164,8 @@ def test_log_probabilities(lib, N):
             assert np.array_equal(f64(c[1])[on], f64(a[1])[on])
 
 
-@pytest.mark.parametrize("N,d,V", [(300, 1168, 50001), (70, 2048, 60000), (1100, 272, 12345), (64, 4624, 30000), (40, 512, 128256)])
+@pytest.mark.parametrize("N,d,V", [(300, 1168, 20001), (70, 2048, 33000), (1100, 272, 12345), (64, 4624, 10000), (40, 512, 128256),
+                                   (300, 1024, 8000), (348, 528, 5000), (3000, 144, 500)])      # small tiles, many of them
 def test_log_probabilities_of_many_tiles(lib, N, d, V):
     x, g = _head(N, d, V, N), _rng(N)
     _check_logprobs(lib, x, g.integers(0, V, N), g.integers(0, 4, N), d, V)
