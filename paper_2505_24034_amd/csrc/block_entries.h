@@ -73,11 +73,12 @@ llamarl_status launch_few(FewArgs a, BlockTile tile, hipStream_t st) {
 }
 template <typename G, typename Out>
 llamarl_status launch_block_logits(BlockLogitsArgs a, hipStream_t st) {
-  a.tiles_v = (int)((a.V + G::Shape::BM - 1) / G::Shape::BM);
+  a.tiles_v = (int)((a.v_end - a.v_first + G::Shape::BM - 1) / G::Shape::BM);
   a.tiles_t = (int)((a.N + G::Shape::BN - 1) / G::Shape::BN);
-  HIP_TRY(set_lds_if_large(k_block_logits<G, Out>, G::LDS_BYTES));
-  k_block_logits<G, Out><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * a.tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS),
-                      G::LDS_BYTES, st>>>(a);
+  constexpr int LDS = G::LDS_BYTES + TileStore<typename G::Shape, Out>::LDS_BYTES;
+  static_assert(LDS * G::GROUPS_PER_CU <= 160 * 1024, "LDS of a CU");
+  HIP_TRY(set_lds_if_large(k_block_logits<G, Out>, LDS));
+  k_block_logits<G, Out><<<dim3((unsigned)persistent_grid((int64_t)a.tiles_v * a.tiles_t, G::GROUPS_PER_CU)), dim3(G::Shape::THREADS), LDS, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
@@ -128,19 +129,26 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   if (s != LLAMARL_OK) return s;
   if (!aligned16(z)) return fail(LLAMARL_ERR_INVALID_ARG, "z must be 16-byte aligned");
   const BlockHead x = block_head(H, H_scale, W, W_scale);
-  const BlockTile tile = block_tile(N, V, z_dt == LLAMARL_F32);
+  const BlockLogits plan = z_dt == LLAMARL_F32 ? BlockLogits{block_tile(N, V, true), V, BLOCK_64} : block_logits(N, V, d);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (tile <= BLOCK_FEW) {
+  if (plan.tile <= BLOCK_FEW) {
     FewArgs f = {};
     f.x = x; f.N = N; f.d = d; f.V = V; f.z = z;
-    return z_dt == LLAMARL_F32 ? launch_few<float>(f, tile, st) : launch_few<uint16_t>(f, tile, st);
+    return z_dt == LLAMARL_F32 ? launch_few<float>(f, plan.tile, st) : launch_few<uint16_t>(f, plan.tile, st);
   }
   BlockLogitsArgs a = {};
-  a.x = x; a.N = N; a.d = d; a.V = V; a.z = z;
-  if (z_dt == LLAMARL_F32) return (tile == BLOCK_64 ? launch_block_logits<Exact64, float> : launch_block_logits<Exact128, float>)(a, st);
-  return (tile == BLOCK_256   ? launch_block_logits<Blocks256, uint16_t>
-          : tile == BLOCK_128 ? launch_block_logits<Blocks128, uint16_t>
-                              : launch_block_logits<Blocks64, uint16_t>)(a, st);
+  a.x = x; a.N = N; a.d = d; a.V = V; a.z = z; a.v_end = plan.rows;
+  if (z_dt == LLAMARL_F32) return (plan.tile == BLOCK_64 ? launch_block_logits<Exact64, float> : launch_block_logits<Exact128, float>)(a, st);
+  const auto launch = [&](BlockTile t) {
+    return (t == BLOCK_256   ? launch_block_logits<Blocks256, uint16_t>
+            : t == BLOCK_128 ? launch_block_logits<Blocks128, uint16_t>
+                             : launch_block_logits<Blocks64, uint16_t>)(a, st);
+  };
+  const llamarl_status first = launch(plan.tile);
+  if (first != LLAMARL_OK || plan.rows == V) return first;
+  a.v_first = plan.rows;
+  a.v_end = V;
+  return launch(plan.rest);
 }
 
 size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) { return N <= 0 || V <= 0 ? 0 : block_ws(N, V).total; }

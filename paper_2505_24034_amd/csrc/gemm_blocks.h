@@ -78,8 +78,7 @@ struct BlockStreams {
   static constexpr int LDS_BYTES = 2 * STAGE;
   static constexpr int GROUPS_PER_CU = Shape::BM == 256 ? 1 : Shape::BM == 128 ? 2 : 4;
   static constexpr int FIRST_PARTS = 4;
-  static constexpr int YOUNGER = MB * NB + LoaderA::ITERS + LoaderB::ITERS + 2;      // see TileGemmBlocks::run
-  static_assert(YOUNGER < 64, "vmcnt counts to 63");
+  static constexpr int SLAB_REQUESTS = LoaderA::ITERS + LoaderB::ITERS + 2;
   static_assert(Shape::WAVE_M <= SCALE_BLOCK && Shape::BN % 64 == 0, "a wavefront's rows share their scales; words of 64 columns a request");
   LoaderA la;
   LoaderB lb;
@@ -259,12 +258,14 @@ struct TileGemmBlocks : BlockStreams<S_, Order_> {
     }
     if (BAR) sc.row = row_next;
   }
-  // counted (wave-uniform): the requests of the first slab were followed by those of the second and by MB * NB stores of the
-  // previous tile, and by no other vector-memory operation: the first slab alone is waited for.
+  // counted (wave-uniform): the requests of the first slab were followed by those of the second and by STORES stores of the
+  // previous tile at least: the first slab alone is waited for.
+  template <int STORES = 0>
   __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {
     const int nk = this->slabs();
     const Addresses ad = Base::addresses();
-    if (counted) wait_vmcnt<Base::YOUNGER>();
+    static_assert(STORES + Base::SLAB_REQUESTS < 64, "vmcnt counts to 63");
+    if (counted) wait_vmcnt<STORES + Base::SLAB_REQUESTS>();
     else wait_vmcnt0();
     __syncthreads();
     frag_t a[4], b[NB];
@@ -372,6 +373,7 @@ struct TileGemmBlocksSimple : BlockStreams<S_, Order_> {
       }
     }
   }
+  template <int STORES = 0>
   __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[MB][NB], bool counted = false) {      // see TileGemmBlocks::run
     const int nk = this->slabs();
     const Addresses ad = Base::addresses();
@@ -379,7 +381,8 @@ struct TileGemmBlocksSimple : BlockStreams<S_, Order_> {
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    if (counted) wait_vmcnt<Base::YOUNGER>();
+    static_assert(STORES + Base::SLAB_REQUESTS < 64, "vmcnt counts to 63");
+    if (counted) wait_vmcnt<STORES + Base::SLAB_REQUESTS>();
     else wait_vmcnt0();
     __syncthreads();
     char *s = smem, *o = smem + Base::STAGE;

@@ -670,6 +670,12 @@ PyObject* block_plan(PyObject* const* a) {
   return Py_BuildValue("iiL", (int)t, llamarl::block_tile_rows(t, integer(a[2])), (long long)llamarl::block_partials(N, V));
 }
 
+// (N, V, d) -> kernel of the first rows of W, how many, kernel of the rest: bf16 logits
+PyObject* block_logits_plan(PyObject* const* a) {
+  const llamarl::BlockLogits p = llamarl::block_logits(integer(a[0]), integer(a[1]), integer(a[2]));
+  return Py_BuildValue("iLi", (int)p.tile, (long long)p.rows, (int)p.rest);
+}
+
 template <PyObject* (*F)(PyObject* const*), int NARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -697,7 +703,7 @@ PyMethodDef g_methods[] = {
     ENTRY(token_logprobs, 6), ENTRY(token_logprobs_partial, 8), ENTRY(merge_partials, 4), ENTRY(offpolicy_loss_fwd, 15),
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
     ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
-    ENTRY(token_logprobs_blocks, 8), ENTRY(block_plan, 4), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(token_logprobs_blocks, 8), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

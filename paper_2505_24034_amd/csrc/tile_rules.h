@@ -281,10 +281,40 @@ constexpr int64_t BLOCK_64_TILES = 128, EXACT_64_TILES = 288;
 LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
   if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
   if (tile_count(N, V, 128) < (exact ? EXACT_64_TILES : BLOCK_64_TILES)) return BLOCK_64;
-  // 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, bf16 logits, us at (N, V, d): (128, 128256, 4096) 127 : 123,
-  // (256, ..) 153 : 194, (300, ..) 211 : 236, (1024, ..) 524 : 667, (1900, 33001, 2048) 160 : 161, (2048, 16032, 8192) 209 : 271, (700, 8000, 1024)
-  // 22 : 15, (1041, 5003, 528) 21 : 13
+  // Log-probs: 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, us at (N, V, d): (128, 128256, 4096) 127 : 123, (256, ..)
+  // 153 : 194, (1024, ..) 524 : 667
   return !exact && N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
+}
+// bf16 logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own.
+struct BlockLogits {
+  BlockTile tile;
+  int64_t rows;
+  BlockTile rest;
+};
+// A round of the grid costs, in ns: 256 x 256 tiles (one on a CU) 14000 + 12.5 d, 128 x 128 ones (two) 7500 + 8.3 d, and two thirds of that where
+// every CU has one at most; a launch 3000; a column of 256 that is half empty or more three quarters.  bf16 logits, us at (N, V, d), 256 x 256 /
+// 128 x 128 / what is picked where it is both: (300, 128256, 4096) 210 / 235, (512, 128256, 2048) 154 / 195, (2000, 65066, 528) 170 / 188,
+// (2048, 16032, 8192) 231 / 295, (323, 43008, 576) 34 / 25, (1096, 28544, 368) 44 / 36, (1900, 33001, 2048) 159 / 184 / 151,
+// (1300, 33024, 1024) 74 / 72 / 66, (1714, 5653, 448) 24.7 / 24.7 / 21.8
+LLAMARL_RULE int64_t block_cost_128(int64_t N, int64_t V, int64_t d) {
+  const int64_t tiles = tile_count(N, V, 128), round = 7500 + 25 * d / 3;
+  return tiles <= 256 ? round * 2 / 3 : (tiles + 511) / 512 * round;
+}
+LLAMARL_RULE BlockLogits block_logits(int64_t N, int64_t V, int64_t d) {
+  const BlockTile t = block_tile(N, V, false);
+  if (t < BLOCK_128) return {t, V, t};
+  const int64_t tiles_t = (N + 255) / 256, tiles = tile_count(N, V, 256), rows = tiles / 256 * 256 / tiles_t * 256;
+  const int64_t round = (14000 + 25 * d / 2) * (4 * tiles_t - ((N - 1) % 256 < 128)) / (4 * tiles_t);
+  BlockLogits best = {BLOCK_128, V, BLOCK_128};
+  int64_t cost = block_cost_128(N, V, d);
+  const int64_t whole = (tiles + 255) / 256 * round;
+  if (whole < cost) {
+    best.tile = BLOCK_256;
+    cost = whole;
+  }
+  if (rows > 0 && rows < V && tiles / 256 * round + block_cost_128(N, V - rows, d) + 3000 < cost)
+    best = {BLOCK_256, rows, tile_count(N, V - rows, 128) < BLOCK_64_TILES ? BLOCK_64 : BLOCK_128};
+  return best;
 }
 // wavefronts of k_few_direct that share rows of W: as many as have a group (512 columns) of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192)
 // 51 / 32 / 32 / 29, (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23

@@ -33,3 +33,15 @@ def test_planes_do_not_shrink(rules):
         assert all(size[a, v] <= size[b, v] for a, b in zip(TOKENS, TOKENS[1:]))
     for n in TOKENS:
         assert all(size[n, a] <= size[n, b] for a, b in zip(VOCAB, VOCAB[1:]))
+
+
+def test_logits_cover_every_row_once(rules):
+    split = 0
+    for N in TOKENS:
+        for V in VOCAB:
+            for d in (16, 528, 2048, 8192):
+                first, rows, rest = rules.block_logits_plan(N, V, d)
+                assert rows == V or (0 < rows < V and rows % 256 == 0 and first == 4 and rest in (2, 3)), (N, V, d)
+                assert first > 1 or N <= (16 if first == 0 else 64)
+                split += rows < V
+    assert split > 0
