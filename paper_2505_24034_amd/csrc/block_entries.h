@@ -107,8 +107,7 @@ llamarl_status llamarl_quantise_blocks(const void* x, int64_t rows, int64_t cols
   if (!aligned16(x) || !aligned16(q)) return fail(LLAMARL_ERR_INVALID_ARG, "x and q must be 16-byte aligned");
   if (!aligned_to(scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "scale must be 4-byte aligned");
   const int64_t groups = (cols + SCALE_GROUP - 1) / SCALE_GROUP, scale_rows = (rows + block_rows - 1) / block_rows;
-  const int64_t x_bytes = rows * cols * (int64_t)esize(dt);
-  if (overlap(x, x_bytes, q, rows * cols) || overlap(x, x_bytes, scale, scale_rows * groups * 4) || overlap(q, rows * cols, scale, scale_rows * groups * 4))
+  if (any_overlap({{q, rows * cols}, {scale, scale_rows * groups * 4}}, {{x, rows * cols * (int64_t)esize(dt)}}))
     return fail(LLAMARL_ERR_INVALID_ARG, "x, q and scale must not overlap");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   QuantiseArgs a = {x, rows, cols, static_cast<uint8_t*>(q), reinterpret_cast<uint32_t*>(scale), (int)groups};
@@ -128,6 +127,10 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   const llamarl_status s = check_block_head(H, H_scale, W, W_scale, N, d, V);
   if (s != LLAMARL_OK) return s;
   if (!aligned16(z)) return fail(LLAMARL_ERR_INVALID_ARG, "z must be 16-byte aligned");
+  const int64_t groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
+  if (any_overlap({{z, N * V * (int64_t)esize(z_dt)}},
+                  {{H, N * d}, {H_scale, groups * N * 4}, {W, V * d}, {W_scale, groups * ((V + SCALE_BLOCK - 1) / SCALE_BLOCK) * 4}}))
+    return fail(LLAMARL_ERR_INVALID_ARG, "z must not overlap an operand");
   const BlockHead x = block_head(H, H_scale, W, W_scale);
   const BlockLogits plan = z_dt == LLAMARL_F32 ? BlockLogits{block_tile(N, V, true), V, BLOCK_64} : block_logits(N, V, d);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
@@ -164,6 +167,11 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
   if (!ws || ws_bytes < w.total)
     return fail(LLAMARL_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws ? ws_bytes : (size_t)0, w.total);
   if (!aligned16(ws)) return fail(LLAMARL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  const int64_t groups = (d + SCALE_GROUP - 1) / SCALE_GROUP;
+  if (any_overlap({{logp, N * 4}, {lse, N * 4}, {ws, (int64_t)w.total}},
+                  {{H, N * d}, {H_scale, groups * N * 4}, {W, V * d}, {W_scale, groups * ((V + SCALE_BLOCK - 1) / SCALE_BLOCK) * 4},
+                   {targets, N * 4}, {mask, N}}))
+    return fail(LLAMARL_ERR_INVALID_ARG, "logp, lse and workspace must not overlap another array");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   char* base = reinterpret_cast<char*>(ws);
   int32_t *rows = reinterpret_cast<int32_t*>(base + w.off_rows), *n_act = reinterpret_cast<int32_t*>(base + w.off_nact);

@@ -423,7 +423,7 @@ struct List {
 // An array of a list's tensor: contiguous, n entries (n < 0: any), on the list's device
 const at::Tensor& listed(const List& l, Py_ssize_t i, int64_t n, std::optional<c10::Device>& device) {
   const at::Tensor& t = tensor(l.at(i), l.name);
-  if (!t.is_cuda() || !t.is_contiguous()) invalid_at(l.name, i, "be a contiguous device tensor");
+  if (!t.is_cuda() || !t.is_contiguous() || t.is_neg()) invalid_at(l.name, i, "be a contiguous device tensor");
   if (n >= 0 && t.numel() != n) invalid_at(l.name, i, "have " + std::to_string(n) + " entries");
   if (!device) device = t.device();
   else if (*device != t.device()) invalid_at(l.name, i, "be on the device of the others");

@@ -43,6 +43,22 @@ llamarl_status for_each_launch(int64_t count, int units, OptList& l, T tensor, F
   return flush();
 }
 
+// Whether a range of what a call writes lies over another of them, or over what it reads.
+struct Span {
+  const void* p;             // null: not given
+  int64_t bytes;
+};
+bool any_overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  auto meet = [](const Span& x, const Span& y) { return x.p != nullptr && y.p != nullptr && overlap(x.p, x.bytes, y.p, y.bytes); };
+  for (const Span* w = written.begin(); w != written.end(); ++w) {
+    for (const Span* o = w + 1; o != written.end(); ++o)
+      if (meet(*w, *o)) return true;
+    for (const Span& r : read)
+      if (meet(*w, r)) return true;
+  }
+  return false;
+}
+
 struct Range {
   uintptr_t from, to;
   int64_t tensor;
@@ -50,8 +66,8 @@ struct Range {
 };
 
 // Whether anything that a step writes lies over something else that it reads or writes.
-llamarl_status check_apart(const llamarl_adamw_tensor* t, int64_t count) {
-  const size_t most = (size_t)count * 7;
+llamarl_status check_apart(const llamarl_adamw_tensor* t, int64_t count, const float* grad_scale, const float* lr_device, const int64_t* step_device) {
+  const size_t most = (size_t)count * 7 + 3;
   Range* r = new (std::nothrow) Range[most];
   if (r == nullptr) return fail(LLAMARL_ERR_INVALID_ARG, "no host memory for a list of %lld tensors", (long long)count);
   size_t k = 0;
@@ -70,6 +86,12 @@ llamarl_status check_apart(const llamarl_adamw_tensor* t, int64_t count) {
     add(t[i].m_scale, blocks * 4, true);
     add(t[i].v_scale, blocks * 4, true);
   }
+  auto word = [&](const void* p, uintptr_t bytes) {
+    if (p != nullptr) r[k++] = {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, count, false};
+  };
+  word(grad_scale, 4);
+  word(lr_device, 4);
+  word(step_device, 8);
   std::sort(r, r + k, [](const Range& x, const Range& y) { return x.from < y.from; });
   int64_t a = -1, b = -1;
   Range read = {0, 0, -1, false}, written = {0, 0, -1, true};        // those that reach furthest so far
@@ -83,12 +105,14 @@ llamarl_status check_apart(const llamarl_adamw_tensor* t, int64_t count) {
     if (r[i].to > far.to) far = r[i];
   }
   delete[] r;
+  if (a == count || b == count)
+    return fail(LLAMARL_ERR_INVALID_ARG, "grad_scale, lr_device or step_device lies in tensor %lld", (long long)std::min(a, b));
   if (a >= 0) return fail(LLAMARL_ERR_INVALID_ARG, "arrays of tensors %lld and %lld overlap", (long long)a, (long long)b);
   return LLAMARL_OK;
 }
 
-llamarl_status check_adamw(const llamarl_adamw_tensor* tensors, int64_t count, const llamarl_adamw_params* p, const float* lr_device,
-                           const int64_t* step_device, int64_t& total) {
+llamarl_status check_adamw(const llamarl_adamw_tensor* tensors, int64_t count, const llamarl_adamw_params* p, const float* grad_scale,
+                           const float* lr_device, const int64_t* step_device, int64_t& total) {
   if (p == nullptr || (tensors == nullptr && count > 0)) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
   if (count < 0 || count > (int64_t)1 << 24) return fail(LLAMARL_ERR_INVALID_ARG, "count must lie in [0, 2^24] (got %lld)", (long long)count);
   auto rate = [](double b) { return b >= 0.0 && b < 1.0; };
@@ -99,7 +123,8 @@ llamarl_status check_adamw(const llamarl_adamw_tensor* tensors, int64_t count, c
     return fail(LLAMARL_ERR_INVALID_ARG, "lr, eps and weight_decay must be finite and not negative (got %g, %g, %g)", p->lr, p->eps,
                 p->weight_decay);
   if (step_device == nullptr && p->step < 1) return fail(LLAMARL_ERR_INVALID_ARG, "step counts from 1 (got %lld)", (long long)p->step);
-  if (!aligned_to(lr_device, 4) || !aligned_to(step_device, 8)) return fail(LLAMARL_ERR_INVALID_ARG, "misaligned lr_device or step_device");
+  if (!aligned_to(grad_scale, 4) || !aligned_to(lr_device, 4) || !aligned_to(step_device, 8))
+    return fail(LLAMARL_ERR_INVALID_ARG, "misaligned grad_scale, lr_device or step_device");
   total = 0;
   for (int64_t i = 0; i < count; ++i) {
     const llamarl_adamw_tensor& t = tensors[i];
@@ -117,7 +142,7 @@ llamarl_status check_adamw(const llamarl_adamw_tensor* tensors, int64_t count, c
     if (t.n > OPT_MAX_ENTRIES || (total += t.n) > OPT_MAX_ENTRIES)
       return fail(LLAMARL_ERR_UNSUPPORTED, "more than 2^34 entries");
   }
-  return check_apart(tensors, count);
+  return check_apart(tensors, count, grad_scale, lr_device, step_device);
 }
 
 }  // namespace
@@ -148,6 +173,12 @@ llamarl_status llamarl_grad_norm(const llamarl_gradient* grads, int64_t count, f
   if (!ws || ws_bytes < need)
     return fail(LLAMARL_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws ? ws_bytes : (size_t)0, need);
   if (!aligned16(ws)) return fail(LLAMARL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+  if (any_overlap({{norm, 4}, {scale, 4}, {ws, (int64_t)need}}, {})) return fail(LLAMARL_ERR_INVALID_ARG, "norm, scale and workspace must not overlap");
+  for (int64_t i = 0; i < count; ++i) {
+    const Span g = {grads[i].n > 0 ? grads[i].grad : nullptr, grads[i].n > 0 ? grads[i].n * (int64_t)esize(grads[i].dt) : 0};
+    if (any_overlap({g}, {{norm, 4}, {scale, 4}, {ws, (int64_t)need}}))
+      return fail(LLAMARL_ERR_INVALID_ARG, "norm, scale or workspace lies in gradient %lld", (long long)i);
+  }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   double* part = reinterpret_cast<double*>(ws);
   // whole units of at least total / NORM_BLOCKS: at most NORM_BLOCKS workgroups, and one more for each tensor's end
@@ -176,9 +207,8 @@ llamarl_status llamarl_grad_norm(const llamarl_gradient* grads, int64_t count, f
 llamarl_status llamarl_adamw_step(const llamarl_adamw_tensor* tensors, int64_t count, const llamarl_adamw_params* p,
                                   const float* grad_scale, const float* lr_device, const int64_t* step_device, void* stream) {
   int64_t total;
-  llamarl_status s = check_adamw(tensors, count, p, lr_device, step_device, total);
+  llamarl_status s = check_adamw(tensors, count, p, grad_scale, lr_device, step_device, total);
   if (s != LLAMARL_OK) return s;
-  if (!aligned_to(grad_scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "misaligned grad_scale");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   AdamwArgs a;
   a.lr = (float)p->lr;

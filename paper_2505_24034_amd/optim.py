@@ -1,5 +1,6 @@
-"""AdamW as a torch optimiser over the library's kernels: `llamarl_grad_norm` and `llamarl_adamw_step` in include/llamarl.h.  One
-or two launches for every 48 tensors, nothing waits for the device, and no arithmetic happens here."""
+"""AdamW as a torch optimiser over the library's kernels: `llamarl_grad_norm` and `llamarl_adamw_step` in include/llamarl.h.  A
+launch for every 48 tensors, another and one more where the norm is asked for; nothing waits for the device, and no arithmetic
+happens here."""
 import torch
 
 from . import binding as L
@@ -10,11 +11,14 @@ class AdamW(torch.optim.Optimizer):
 
     state_bits      32, or 8: a quarter of the memory (binding.adamw_step says how they are held)
     master_weights  keep a float32 copy of bfloat16 parameters, which is what moves; without it changes below half a
-                    parameter's last bit are lost
+                    parameter's last bit are lost.  It is taken at the parameter's first step: weights that are loaded later have to
+                    come with the optimiser's state
     max_grad_norm   scale the gradients of all groups down to this norm; `grad_norm` then holds the norm before it (one
-                    element, on the device).  A norm that is not finite leaves every parameter and state as it was
+                    element, on the device).  A norm that is not finite leaves every parameter and state as it was (the step is
+                    counted); without max_grad_norm nothing looks for such gradients
 
-    lr, betas, eps, weight_decay are read from the groups at every step, as schedulers set them."""
+    lr, betas, eps, weight_decay are read from the groups at every step, as schedulers set them; lr may be a tensor (one on the
+    GPU is read there, when the kernels run)."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master_weights=True,
                  max_grad_norm=None):
@@ -22,6 +26,11 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError("state_bits must be 8 or 32 (got %r)" % (state_bits,))
         self.state_bits, self.master_weights, self.max_grad_norm, self.grad_norm = state_bits, master_weights, max_grad_norm, None
         super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+
+    def __getstate__(self):
+        """As torch's, which would leave out what it does not know."""
+        own = ("state_bits", "master_weights", "max_grad_norm", "grad_norm")
+        return {**super().__getstate__(), **{name: getattr(self, name) for name in own}}
 
     def _init_state(self, p):
         s = self.state[p]
@@ -65,9 +74,12 @@ class AdamW(torch.optim.Optimizer):
             self.grad_norm, scale = L.grad_norm([g for pairs in runs.values() for _, g in pairs], self.max_grad_norm)
         for (i, step), pairs in runs.items():
             group, states = self.param_groups[i], [self.state[p] for p, _ in pairs]
+            lr = group["lr"]
+            if torch.is_tensor(lr) and not lr.is_cuda:
+                lr = float(lr)
             def column(name):
                 return [s.get(name) for s in states]
-            L.adamw_step([p for p, _ in pairs], [g for _, g in pairs], column("exp_avg"), column("exp_avg_sq"), group["lr"], step,
+            L.adamw_step([p for p, _ in pairs], [g for _, g in pairs], column("exp_avg"), column("exp_avg_sq"), lr, step,
                          betas=group["betas"], eps=group["eps"], weight_decay=group["weight_decay"], masters=column("master"),
                          exp_avg_scales=column("exp_avg_scale"), exp_avg_sq_scales=column("exp_avg_sq_scale"), grad_scale=scale)
             for s in states:

@@ -286,3 +286,22 @@ def test_on_a_stream_of_its_own(lib):
         torch.cuda.synchronize()
         for a, b in zip(got, want):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_two_streams_at_once(lib):
+    """calls whose workspaces and outputs are their own: as one after the other"""
+    calls = []
+    for i, N in enumerate((700, 40, 650, 30)):
+        x = _head(N, 528, 5000, 40 + i)
+        t = torch.from_numpy(_rng(i).integers(0, 5000, N).astype(np.int32)).cuda()
+        calls.append((x, t, lib.token_logprobs_blocks(*x, t), lib.logits_blocks(*x)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for turn in range(3):
+        for i, (x, t, _, _) in enumerate(calls):
+            with torch.cuda.stream(streams[i % 2]):
+                got.append((i, lib.token_logprobs_blocks(*x, t), lib.logits_blocks(*x)))
+    torch.cuda.synchronize()
+    for i, (logp, lse), z in got:
+        assert torch.equal(logp, calls[i][2][0]) and torch.equal(lse, calls[i][2][1]) and torch.equal(z, calls[i][3])

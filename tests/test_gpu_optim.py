@@ -448,3 +448,14 @@ class TestOptimiser:
         ps[2].grad = torch.randn(64, 128, device="cuda").T                 # a gradient in another order than its parameter
         opt.step()
         assert torch.isfinite(ps[2]).all() and not torch.equal(ps[2], before[2])
+
+    def test_rate_as_a_tensor(self, lib):
+        from paper_2505_24034_amd.optim import AdamW
+        for rate in (torch.tensor(1e-2), torch.tensor([1e-2], device="cuda")):
+            ps, qs = self._model(torch.float32), self._model(torch.float32)
+            a, b = AdamW(ps, lr=float(torch.tensor(1e-2))), AdamW(qs, lr=rate)
+            for t in range(2):
+                for x, o in ((ps, a), (qs, b)):
+                    self._gradients(x, t)
+                    o.step()
+            assert all(torch.equal(p, q) for p, q in zip(ps, qs))

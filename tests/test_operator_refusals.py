@@ -1,4 +1,5 @@
 """What the optimiser step and the 8-bit head refuse, without a GPU: every check comes before anything is launched."""
+import copy
 import ctypes
 
 import pytest
@@ -173,3 +174,34 @@ def test_optimiser_refuses():
     with pytest.raises(ValueError):
         AdamW([p], state_bits=16)
     assert AdamW([p]).step() is None                                       # no gradient: nothing to do
+
+
+@no_gpu_only
+def test_outputs_do_not_lie_over_operands(clib):
+    vp = ctypes.c_void_p
+    a = _tensor()
+    for kw in (dict(scale=vp(a.param + 996 * 4 + 12)), dict(lr_device=vp(a.v)), dict(step_device=vp(a.m + 8))):
+        assert _adamw(clib, _tensor(1 << 28), a, **kw) == L.ERR_INVALID_ARG
+        assert b"lies in tensor 1" in clib.llamarl_last_error()
+    g = (L.Gradient * 2)(L.Gradient(1 << 20, 10, L.BF16), L.Gradient(1 << 24, 100, L.F32))
+    for norm, scale, ws in ((1 << 10, 1 << 10, 1 << 12), (1 << 10, 1 << 12, 1 << 12), ((1 << 24) + 396, 1 << 11, 1 << 12),
+                            (1 << 10, (1 << 20) + 16, 1 << 12), (1 << 10, 1 << 11, (1 << 24) - 16)):
+        assert clib.llamarl_grad_norm(g, 2, 1.0, vp(norm), vp(scale), vp(ws), 1 << 20, None) == L.ERR_INVALID_ARG
+        assert b"norm" in clib.llamarl_last_error()
+    H, Hs, W, Ws, N, d, V = 1 << 24, 1 << 25, 1 << 26, 1 << 27, 10, 64, 50
+    for z in (H, H + 624, Hs + 32, W - 16, W + 50 * 64 - 16, Ws):
+        assert clib.llamarl_logits_blocks(vp(H), vp(Hs), vp(W), vp(Ws), N, d, V, L.F32, vp(z), None) == L.ERR_INVALID_ARG
+        assert b"overlap" in clib.llamarl_last_error()
+    tg, mask = 1 << 28, 1 << 29
+    for logp, lse, ws in ((1 << 30, 1 << 30, 1 << 31), (tg + 36, 1 << 30, 1 << 31), (1 << 30, mask + 8, 1 << 31), (1 << 30, 1 << 32, 1 << 30),
+                          (1 << 30, 1 << 32, W)):
+        assert clib.llamarl_token_logprobs_blocks(vp(H), vp(Hs), vp(W), vp(Ws), vp(tg), vp(mask), N, d, V, vp(logp), vp(lse), vp(ws), 1 << 20,
+                                                  None) == L.ERR_INVALID_ARG
+        assert b"overlap" in clib.llamarl_last_error()
+
+
+def test_optimiser_is_copied_whole():
+    opt = AdamW([torch.nn.Parameter(torch.zeros(4))], state_bits=8, master_weights=False, max_grad_norm=2.0)
+    twin = copy.deepcopy(opt)
+    assert (twin.state_bits, twin.master_weights, twin.max_grad_norm, twin.grad_norm) == (8, False, 2.0, None)
+    assert twin.step() is None
