@@ -176,56 +176,29 @@ struct BlockLogitsArgs {
   int tiles_v, tiles_t;
   void* z;                 // [N][V]
 };
-// A tile's accumulators to z (its first logit), after(j) behind column block j.  STORES: of a wavefront of a whole tile, at least.
-// LDS_BYTES: of a workgroup's, behind the slabs.
+// A tile's accumulators to z (its first logit), after(j) behind column block j.  Through a corner of LDS that the wavefront has for itself,
+// 16 tokens x 128 bytes at a time, so that an instruction writes 128 bytes of a token: straight from the registers 32 of bf16, which took
+// (2000, 65066, 528) 185 us instead of 173, (1714, 5653, 448) 28.4 instead of 24.8, and 64 of fp32: (2000, 65066, 528) 310
+// instead of 295.
+typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(2)));      // rows of z start wherever V puts them
 template <typename S, typename Out>
-struct TileStore;
-// fp32: four neighbouring logits of a token a store, 64 bytes of a token an instruction; buffer stores, whose lanes past the matrix are
-// put out of bounds: one offset a column is all that they keep in registers.
-template <typename S>
-struct TileStore<S, float> {
-  static constexpr int STORES = S::MB * S::NB, LDS_BYTES = 0;
+struct TileStore {
+  static constexpr bool BF16_OUT = sizeof(Out) == 2;
+  // logits of a lane's store, and of 128 bytes (64 x 64 tiles: 64, all that four of them leave of a CU's LDS)
+  static constexpr int PER = 16 / (int)sizeof(Out), MOST = (S::BM == 64 ? 4 : 8) * PER;
+  static constexpr int PART = S::WAVE_M < MOST ? S::WAVE_M : MOST, BLOCKS = PART / 16;      // logits of a token, row blocks of a part
+  static constexpr int PITCH = PART * (int)sizeof(Out) + 16, LANES = PART / PER;            // bytes of a token's row in LDS; lanes that store it
+  static constexpr int EACH = 16 * LANES / 64;                             // stores of a part
+  static constexpr int STORES = S::NB * (S::WAVE_M / PART) * EACH;         // of a wavefront of a whole tile, at least
+  static constexpr int LDS_BYTES = S::WAVES * 16 * PITCH;                  // of a workgroup, behind the slabs
   template <typename F>
-  __device__ __forceinline__ static void run(float* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT,
-                                             char*, F after) {
+  __device__ __forceinline__ static void run(Out* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT,
+                                             char* lds, F after) {
+    char* own = lds + wave_id() * 16 * PITCH;
     const uint64_t p = reinterpret_cast<uint64_t>(z);
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p) |
                                                                              (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32)) << 32),
                                                       (short)0, 0x7fffffff, 0x00020000);
-#pragma unroll
-    for (int j = 0; j < S::NB; ++j) {
-      const uint32_t at = lp.col(j) < rowsT ? ((uint32_t)lp.col(j) * (uint32_t)V + (uint32_t)lp.row(0, 0)) * 4u : OOB_OFFSET;
-      if (rowsV == S::BM) {                          // block-uniform
-#pragma unroll
-        for (int i = 0; i < S::MB; ++i)
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4_t, acc[i][j]), rs, (int)at, 64 * i, 0);
-      } else {
-#pragma unroll
-        for (int i = 0; i < S::MB; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[i][j][r]), rs, (int)(lp.row(i, r) < rowsV ? at : OOB_OFFSET), 64 * i + 4 * r, 0);
-      }
-      LLAMARL_FENCE();
-      after(j);
-      LLAMARL_FENCE();
-    }
-  }
-};
-// bf16: through a corner of LDS that the wavefront has for itself, 16 tokens x 64 logits at a time, so that an instruction writes 128 bytes
-// of a token: straight from the registers 32, and which took (2000, 65066, 528)
-// 185 us instead of 173, (1714, 5653, 448) 28.4 instead of 24.8.
-typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(2)));      // rows of z start wherever V puts them
-template <typename S>
-struct TileStore<S, uint16_t> {
-  static constexpr int PART = S::WAVE_M < 64 ? S::WAVE_M : 64, BLOCKS = PART / 16;      // logits of a token, row blocks of a part
-  static constexpr int PITCH = PART * 2 + 16, LANES = PART / 8;                         // bytes of a token's row in LDS; lanes that store it
-  static constexpr int EACH = 16 * LANES / 64;                                          // stores of a part
-  static constexpr int STORES = S::NB * (S::WAVE_M / PART) * EACH, LDS_BYTES = S::WAVES * 16 * PITCH;
-  template <typename F>
-  __device__ __forceinline__ static void run(uint16_t* z, int64_t V, const f32x4_t (&acc)[S::MB][S::NB], const LanePos<S>& lp, int rowsV, int rowsT,
-                                             char* lds, F after) {
-    char* own = lds + wave_id() * 16 * PITCH;
     const int l16 = lp.lane & 15, g = lp.lane >> 4, token = lp.lane / LANES, chunk = lp.lane % LANES;
 #pragma unroll
     for (int j = 0; j < S::NB; ++j) {
@@ -233,25 +206,41 @@ struct TileStore<S, uint16_t> {
       for (int part = 0; part < S::WAVE_M / PART; ++part) {
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
-          uint16_t b[4];
+          const f32x4_t x = acc[part * BLOCKS + i][j];
+          char* at = own + l16 * PITCH + (16 * i + 4 * g) * (int)sizeof(Out);
+          if constexpr (BF16_OUT) {
+            uint16_t b[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) b[r] = float_to_bf16_bits(acc[part * BLOCKS + i][j][r]);
-          *reinterpret_cast<u32x2*>(own + l16 * PITCH + (16 * i + 4 * g) * 2) = u32x2{(uint32_t)b[0] | (uint32_t)b[1] << 16, (uint32_t)b[2] | (uint32_t)b[3] << 16};
+            for (int r = 0; r < 4; ++r) b[r] = float_to_bf16_bits(x[r]);
+            *reinterpret_cast<u32x2*>(at) = u32x2{(uint32_t)b[0] | (uint32_t)b[1] << 16, (uint32_t)b[2] | (uint32_t)b[3] << 16};
+          } else {
+            *reinterpret_cast<f32x4_t*>(at) = x;
+          }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // a wavefront's LDS operations stay in order
 #pragma unroll
         for (int e = 0; e < EACH; ++e) {
-          const int t = e * (64 / LANES) + token, v = lp.wm * S::WAVE_M + part * PART + chunk * 8;
+          const int t = e * (64 / LANES) + token, v = lp.wm * S::WAVE_M + part * PART + chunk * PER;
           const i32x4_t w = *reinterpret_cast<const i32x4_t*>(own + t * PITCH + chunk * 16);
           const int col = lp.wn * S::WAVE_N + 16 * j + t;
-          if (col < rowsT) {
-            uint16_t* at = z + (int64_t)col * V + v;
-            if (v + 8 <= rowsV) {
-              *reinterpret_cast<i32x4_any*>(at) = i32x4_any{w[0], w[1], w[2], w[3]};
+          if constexpr (BF16_OUT) {
+            if (col < rowsT) {
+              Out* at = z + (int64_t)col * V + v;
+              if (v + PER <= rowsV) {
+                *reinterpret_cast<i32x4_any*>(at) = i32x4_any{w[0], w[1], w[2], w[3]};
+              } else {
+#pragma unroll
+                for (int r = 0; r < PER - 1; ++r)
+                  if (v + r < rowsV) at[r] = (uint16_t)((uint32_t)w[r / 2] >> 16 * (r % 2));
+              }
+            }
+          } else {                                   // lanes past the matrix out of bounds: one offset is all that the stores keep in registers
+            const uint32_t at = col < rowsT ? ((uint32_t)col * (uint32_t)V + (uint32_t)v) * 4u : OOB_OFFSET;
+            if (rowsV == S::BM) {                    // block-uniform
+              __builtin_amdgcn_raw_buffer_store_b128(w, rs, (int)at, 0, 0);
             } else {
 #pragma unroll
-              for (int r = 0; r < 7; ++r)
-                if (v + r < rowsV) at[r] = (uint16_t)((uint32_t)w[r / 2] >> 16 * (r % 2));
+              for (int r = 0; r < 4; ++r) __builtin_amdgcn_raw_buffer_store_b32((uint32_t)w[r], rs, (int)(v + r < rowsV ? at : OOB_OFFSET), 4 * r, 0);
             }
           }
         }
