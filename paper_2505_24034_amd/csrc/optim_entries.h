@@ -181,8 +181,10 @@ llamarl_status llamarl_grad_norm(const llamarl_gradient* grads, int64_t count, f
   }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   double* part = reinterpret_cast<double*>(ws);
-  // whole units of at least total / NORM_BLOCKS: at most NORM_BLOCKS workgroups, and one more for each tensor's end
-  const int units = (int)std::max<int64_t>((total + (int64_t)NORM_BLOCKS * OPT_UNIT - 1) / ((int64_t)NORM_BLOCKS * OPT_UNIT), 1);
+  // Whole units of at least total / NORM_BLOCKS, in turns of NORM_LOADS: at most NORM_BLOCKS workgroups, and one more for each tensor's end.  4096 /
+  // 8192 / 16384 / 32768 of them: 170 M model in bf16 69 / 69 / 67 / 88 us, fp32 130 / 127 / 127 / 124; 525 M entries in fp32 360 / 349 / 352 / 372.
+  int units = (int)std::max<int64_t>((total + (int64_t)NORM_BLOCKS * OPT_UNIT - 1) / ((int64_t)NORM_BLOCKS * OPT_UNIT), 1);
+  if (units > 2) units = (units + NORM_LOADS - 1) / NORM_LOADS * NORM_LOADS;
   OptList l;
   int64_t done = 0;
   const llamarl_status s = for_each_launch(

@@ -30,7 +30,7 @@ constexpr int OPT_THREADS = 512, OPT_ITEMS = 8, OPT_UNIT = OPT_THREADS * OPT_ITE
 constexpr int STATE_BLOCK = 128;             // 16 lanes of eight entries: one row of a wavefront's cross-lane moves
 constexpr float E4M3_MAX = 448.f;
 constexpr float STATE_TINY = 0x1p-100f;      // a block whose largest magnitude is below this is held as zeros (its inverse overflows)
-constexpr int NORM_BLOCKS = 4096;            // partial sums of a gradient norm: at most so many and one a tensor
+constexpr int NORM_BLOCKS = 8192;            // partial sums of a gradient norm: at most so many and one a tensor
 
 enum OptFlags { OPT_P_BF16 = 1, OPT_G_BF16 = 2, OPT_8BIT = 4, OPT_WIDE = 8 /* 16-byte accesses of every array are aligned */ };
 struct OptTensor {
@@ -119,19 +119,52 @@ __device__ __forceinline__ void store8(uint16_t* x, int64_t at, int left, bool w
 
 // ---- norm ------------------------------------------------------------------------------------------------------------------
 // Squares and sums in 64 bits: no entry's square overflows or vanishes, and the order of half a billion additions does not show.
+__device__ __forceinline__ double add_squares(const float (&x)[OPT_ITEMS], double s) {
+#pragma unroll
+  for (int i = 0; i < OPT_ITEMS; ++i) s = fma((double)x[i], (double)x[i], s);
+  return s;
+}
+// Whole units of an aligned tensor, NORM_LOADS of them asked for before the first is used: one at a time leaves few
+// bytes in flight where the gradients are bf16.  109 tensors of a 170 M model, bf16 79.7 -> 69.4 us, fp32 132 -> 127; 525 M entries 185 -> 183, 358 -> 349.
+constexpr int NORM_LOADS = 4;
+template <typename T>
+__device__ __forceinline__ double unit_squares(const T* g, int64_t at, double s) {
+  constexpr int WORDS = OPT_ITEMS * (int)sizeof(T) / 16;
+  i32x4_t w[NORM_LOADS][WORDS];
+#pragma unroll
+  for (int q = 0; q < NORM_LOADS; ++q)
+#pragma unroll
+    for (int c = 0; c < WORDS; ++c) w[q][c] = *reinterpret_cast<const i32x4_t*>(g + at + (int64_t)q * OPT_UNIT + c * (16 / sizeof(T)));
+#pragma unroll
+  for (int q = 0; q < NORM_LOADS; ++q) {
+    float x[OPT_ITEMS];
+#pragma unroll
+    for (int i = 0; i < OPT_ITEMS; ++i) {
+      if constexpr (sizeof(T) == 4) x[i] = __uint_as_float((uint32_t)w[q][i / 4][i % 4]);
+      else x[i] = __uint_as_float(i % 2 == 0 ? (uint32_t)w[q][0][i / 2] << 16 : (uint32_t)w[q][0][i / 2] & 0xffff0000u);
+    }
+    s = add_squares(x, s);
+  }
+  return s;
+}
 __global__ __launch_bounds__(OPT_THREADS) void k_grad_squares(OptList l, double* part) {
   const int t = opt_tensor_of(l);
   const int64_t n = l.t[t].n, from = (int64_t)((int)blockIdx.x - l.first[t]) * l.units * OPT_UNIT;
   const bool bf16 = (l.t[t].flags & OPT_G_BF16) != 0, wide = (l.t[t].flags & OPT_WIDE) != 0;
   const void* g = l.t[t].g;
   double s = 0.0;
-  for (int u = 0; u < l.units; ++u) {
+  int u = 0;
+  if (wide)                                          // uniform, as is the loop's end
+    for (; u + NORM_LOADS <= l.units && from + (int64_t)(u + NORM_LOADS) * OPT_UNIT <= n; u += NORM_LOADS) {
+      const int64_t at = from + (int64_t)u * OPT_UNIT + threadIdx.x * OPT_ITEMS;
+      s = bf16 ? unit_squares(static_cast<const uint16_t*>(g), at, s) : unit_squares(static_cast<const float*>(g), at, s);
+    }
+  for (; u < l.units; ++u) {
     const int64_t at = from + (int64_t)u * OPT_UNIT + threadIdx.x * OPT_ITEMS;
     if (at >= n) break;
     float x[OPT_ITEMS];
     load8(g, bf16, at, (int)min(n - at, (int64_t)OPT_ITEMS), wide, x);
-#pragma unroll
-    for (int i = 0; i < OPT_ITEMS; ++i) s = fma((double)x[i], (double)x[i], s);
+    s = add_squares(x, s);
   }
   __shared__ double s_w[OPT_THREADS / 64];
   s = wave_sum(s);
