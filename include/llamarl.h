@@ -8,6 +8,11 @@
  *                                  rho, advantage weighting, masked means
  *   3. llamarl_offpolicy_loss_bwd  gradients w.r.t. hidden states and LM head
  *
+ * and what stands on either side of it: llamarl_grad_norm and
+ * llamarl_adamw_step apply a model's gradients; llamarl_quantise_blocks,
+ * llamarl_logits_blocks and llamarl_token_logprobs_blocks are the head in 8
+ * bits, as a generator uses it between two updates.
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  *  - All data pointers are DEVICE pointers (HIP global memory on the current
@@ -22,7 +27,8 @@
  *    llamarl_last_error() then returns a message (thread-local storage).
  *    LLAMARL_ERR_HIP (a launch the runtime refused) can come after earlier
  *    kernels of the same call were enqueued: outputs are then undefined.
- *  - Pointers must be 16-byte aligned (anything hipMalloc/torch returns is).
+ *  - Pointers must be 16-byte aligned (anything hipMalloc/torch returns is)
+ *    where an entry point does not say that less will do.
  *  - dtype LLAMARL_BF16 needs d % 8 == 0, LLAMARL_F32 needs d % 4 == 0
  *    (16-byte rows).  N, V are arbitrary (>= 1).  W may exceed 4 GiB; H must be
  *    smaller than 2 GiB (its rows are gathered with 32-bit offsets) and a
