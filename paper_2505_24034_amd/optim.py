@@ -87,10 +87,10 @@ class AdamW(torch.optim.Optimizer):
         return loss
 
     def load_state_dict(self, state_dict):
-        """As torch's, which would turn the states into the parameters' type."""
+        """As torch's, which would turn the states into the parameters' type.  float32 states of torch.optim.AdamW can be gone on from."""
         super().load_state_dict(state_dict)
         saved = [k for group in state_dict["param_groups"] for k in group["params"]]
         for k, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
             if k in state_dict["state"]:
-                self.state[p] = {name: v.detach().to(p.device, copy=True) if torch.is_tensor(v) else v
+                self.state[p] = {name: int(v) if name == "step" else v.detach().to(p.device, copy=True) if torch.is_tensor(v) else v
                                  for name, v in state_dict["state"][k].items()}

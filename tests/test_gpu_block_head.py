@@ -305,3 +305,15 @@ def test_two_streams_at_once(lib):
     torch.cuda.synchronize()
     for i, (logp, lse), z in got:
         assert torch.equal(logp, calls[i][2][0]) and torch.equal(lse, calls[i][2][1]) and torch.equal(z, calls[i][3])
+
+
+@pytest.mark.parametrize("N", [5, 40, 130, 700])
+def test_scratch_is_written_before_it_is_read(lib, N):
+    x, g = _head(N, 528, 5000, N), _rng(N)
+    t, m = torch.from_numpy(g.integers(0, 5000, N).astype(np.int32)).cuda(), torch.from_numpy(g.integers(0, 2, N).astype(np.uint8)).cuda()
+    want = lib.token_logprobs_blocks(*x, t, m)
+    size = lib.logprobs_blocks_workspace_bytes(N, 5000)
+    for fill in (0xFF, 0x7F, 0):
+        ws = torch.full((size + 64,), fill, dtype=torch.uint8, device="cuda")
+        got = lib.token_logprobs_blocks(*x, t, m, ws=ws[:size])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and bool((ws[size:] == fill).all())

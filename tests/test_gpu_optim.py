@@ -459,3 +459,22 @@ class TestOptimiser:
                     self._gradients(x, t)
                     o.step()
             assert all(torch.equal(p, q) for p, q in zip(ps, qs))
+
+    def test_goes_on_from_torchs_states(self, lib):
+        from paper_2505_24034_amd.optim import AdamW
+        ps, qs = self._model(torch.float32), self._model(torch.float32)
+        theirs, ours = torch.optim.AdamW(ps, lr=1e-2, weight_decay=0.1), AdamW(qs, lr=1e-2, weight_decay=0.1)
+        for t in range(4):
+            if t == 2:
+                for p, q in zip(ps, qs):
+                    q.data.copy_(p.data)
+                ours.load_state_dict(theirs.state_dict())
+            self._gradients(ps, t)
+            theirs.step()
+            if t >= 2:
+                self._gradients(qs, t)
+                ours.step()
+        for p, q in zip(ps, qs):
+            # two steps of at most 1.1 lr each, every one within 40 u of itself on either side, and two roundings a step
+            assert (np.abs(f64(p) - f64(q)) <= 2 * (80 * U * 1.1e-2 + 2 * U * (np.abs(f64(p)) + 1.1e-2))).all()
+            assert ours.state[q]["step"] == 4
