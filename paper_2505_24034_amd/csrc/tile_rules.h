@@ -271,15 +271,20 @@ constexpr int DIRECT_WAVES = 8, FEW_ROWS = 64;
 //   (16, 5003, 1024)          6.2 / 6.2 / 13.6                                7.4,  18 : 6.2
 //   (8, 1000, 8192)           8.8 / 18.7 / 81                                  32,  50 : 19
 //   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
-// So tiles of 128 rows where there is one for every CU (fp32 ones: two), below that the direct kernel for up to four tokens and for few
-// rows, the one through LDS to 64 tokens.
+// So tiles where there is one of 128 rows for every CU (fp32 ones: two), though most such calls then take 64 x 64 ones (below), else the
+// direct kernel for up to four tokens and for few rows, the one through LDS to 64 tokens.
 enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_64, BLOCK_128, BLOCK_256 };
 // Fewer tiles of 128 x 128 than this are cut into 64 x 64.  us at (N, V, d), 128 / 64, fp32 | bf16: (100, 4346, 1104) 18 / 9.0 | 9.9 / 6.5,
 // (200, 1000, 4096) 48 / 21 | 20 / 13, (100, 16032, 8192) 85 / 52 | 45 / 35, (300, 8000, 1024) 18.3 / 14.5 | 10.7 / 10.2 (log-probs 16.9 / 18.2),
 // (128, 33001, 4096) 67 / 53 | 36 / 39, (1041, 5003, 528) 18.6 / 22.3 | 13.4 / 19.1
-constexpr int64_t BLOCK_64_TILES = 128, EXACT_64_TILES = 288;
+// FEW: with up to 64 tokens, whose tiles wait for W, four small ones on a CU ask for as much and are spread more evenly.  bf16 | fp32
+// logits, 128 / 64: (43, 44347, 4688) 75 / 67 (log-probs 84 / 75), (64, 33001, 2048) 23.7 / 20.1, (20, 66000, 4096) 89 / 75 | 96 / 77, (30, 70000, 4096)
+// 91 / 82 | 102 / 87, (1, 40000, 8192) 95 / 64 (102 / 72), (1, 128256, 4096) 108 / 105 | 108 / 103; (48, 128256, 4096) 117 / 117 | 118 / 129,
+// (64, 128256, 8192) 217 / 228 | 223 / 244
+constexpr int64_t BLOCK_64_TILES = 128, EXACT_64_TILES = 288, FEW_64_TILES = 768;
 LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
   if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
+  if (N <= FEW_TOKENS && (N <= 4 || tile_count(N, V, 128) < FEW_64_TILES)) return BLOCK_64;
   if (tile_count(N, V, 128) < (exact ? EXACT_64_TILES : BLOCK_64_TILES)) return BLOCK_64;
   // Log-probs: 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, us at (N, V, d): (128, 128256, 4096) 127 : 123, (256, ..)
   // 153 : 194, (1024, ..) 524 : 667
