@@ -271,7 +271,7 @@ constexpr int DIRECT_WAVES = 8, FEW_ROWS = 64;
 //   (16, 5003, 1024)          6.2 / 6.2 / 13.6                                7.4,  18 : 6.2
 //   (8, 1000, 8192)           8.8 / 18.7 / 81                                  32,  50 : 19
 //   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
-// So tiles where there is one of 128 rows for every CU (fp32 ones: two), though most such calls then take 64 x 64 ones (below), else the
+// (tiles of 128 x 128).  So tiles where there is one of those for every CU, though most such calls then take 64 x 64 ones (below), else the
 // direct kernel for up to four tokens and for few rows, the one through LDS to 64 tokens.
 enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_64, BLOCK_128, BLOCK_256 };
 // Fewer tiles of 128 x 128 than this are cut into 64 x 64.  us at (N, V, d), 128 / 64, fp32 | bf16: (100, 4346, 1104) 18 / 9.0 | 9.9 / 6.5,
@@ -280,10 +280,11 @@ enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_64, BLOCK_128, BLOCK_256 };
 // FEW: with up to 64 tokens, whose tiles wait for W, four small ones on a CU ask for as much and are spread more evenly.  bf16 | fp32
 // logits, 128 / 64: (43, 44347, 4688) 75 / 67 (log-probs 84 / 75), (64, 33001, 2048) 23.7 / 20.1, (20, 66000, 4096) 89 / 75 | 96 / 77, (30, 70000, 4096)
 // 91 / 82 | 102 / 87, (1, 40000, 8192) 95 / 64 (102 / 72), (1, 128256, 4096) 108 / 105 | 108 / 103; (48, 128256, 4096) 117 / 117 | 118 / 129,
-// (64, 128256, 8192) 217 / 228 | 223 / 244
+// (64, 128256, 8192) 217 / 228 | 223 / 244.  fp32, kernels for few tokens / 64 x 64: (10, 16032, 4096) 17 / 25, (48, 24000, 4096) 37 / 38, (3, 33001, 2048)
+// 19 / 21, (10, 33001, 2048) 25 / 21, (48, 33001, 2048) 33 / 26, (64, 50000, 8192) 144 / 112, (48, 60000, 512) 30 / 16
 constexpr int64_t BLOCK_64_TILES = 128, EXACT_64_TILES = 288, FEW_64_TILES = 768;
 LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
-  if (N <= FEW_TOKENS && V <= (exact ? 512 : 256) * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
+  if (N <= FEW_TOKENS && V <= 256 * 128 - 128) return N <= 4 || (N <= DIRECT_TOKENS && V < 8192) ? BLOCK_DIRECT : BLOCK_FEW;
   if (N <= FEW_TOKENS && (N <= 4 || tile_count(N, V, 128) < FEW_64_TILES)) return BLOCK_64;
   if (tile_count(N, V, 128) < (exact ? EXACT_64_TILES : BLOCK_64_TILES)) return BLOCK_64;
   // Log-probs: 256 x 256 tiles (128 tokens or fewer leave half of one empty) : 128 x 128, us at (N, V, d): (128, 128256, 4096) 127 : 123, (256, ..)

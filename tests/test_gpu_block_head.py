@@ -110,7 +110,8 @@ def test_logits(lib, i, N, dtype):
 @pytest.mark.parametrize("N,d,V,dtype", [(300, 1168, 20001, torch.bfloat16), (70, 2048, 33000, torch.bfloat16), (1100, 272, 12345, torch.bfloat16),
                                          (64, 4624, 10000, torch.float32), (150, 656, 20011, torch.float32), (2000, 128, 8200, torch.bfloat16),
                                          (300, 1024, 8000, torch.float32), (300, 1024, 8000, torch.bfloat16), (3000, 144, 500, torch.bfloat16),
-                                         (430, 144, 32969, torch.bfloat16), (530, 144, 26309, torch.bfloat16)])
+                                         (430, 144, 32969, torch.bfloat16), (530, 144, 26309, torch.bfloat16),
+                                         (40, 272, 33000, torch.float32), (3, 144, 40001, torch.float32), (64, 1040, 32641, torch.bfloat16)])
 def test_logits_of_many_tiles(lib, N, d, V, dtype):
     """more tiles than workgroups, turned slabs (few columns of tiles), every kernel's last tile in both directions, the last rows of W on smaller tiles
     (two kinds)"""
