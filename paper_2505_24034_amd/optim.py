@@ -18,7 +18,8 @@ class AdamW(torch.optim.Optimizer):
                     counted); without max_grad_norm nothing looks for such gradients
 
     lr, betas, eps, weight_decay are read from the groups at every step, as schedulers set them; lr may be a tensor (one on the
-    GPU is read there, when the kernels run)."""
+    GPU is read there, when the kernels run).  Groups of torch.optim.Adam and AdamW with amsgrad, maximize or a decay inside the
+    gradient are refused."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, master_weights=True,
                  max_grad_norm=None):
@@ -31,6 +32,18 @@ class AdamW(torch.optim.Optimizer):
         """As torch's, which would leave out what it does not know."""
         own = ("state_bits", "master_weights", "max_grad_norm", "grad_norm")
         return {**super().__getstate__(), **{name: getattr(self, name) for name in own}}
+
+    def add_param_group(self, param_group):
+        self._check_group(param_group)
+        super().add_param_group(param_group)
+
+    def _check_group(self, group):
+        """torch's settings that change the step and are not computed here"""
+        set_ = [name for name in ("amsgrad", "maximize") if group.get(name)]
+        if not group.get("decoupled_weight_decay", True) and group.get("weight_decay", self.defaults["weight_decay"]):
+            set_.append("decoupled_weight_decay=False")
+        if set_:
+            raise L.LlamarlError(L.ERR_UNSUPPORTED, "a parameter group with " + ", ".join(set_))
 
     def _init_state(self, p):
         s = self.state[p]
@@ -88,6 +101,8 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         """As torch's, which would turn the states into the parameters' type.  float32 states of torch.optim.AdamW can be gone on from."""
+        for group in state_dict["param_groups"]:
+            self._check_group(group)
         super().load_state_dict(state_dict)
         saved = [k for group in state_dict["param_groups"] for k in group["params"]]
         for k, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):

@@ -1,0 +1,53 @@
+"""What `optim.AdamW` takes from a checkpoint, and what it refuses: no kernel runs."""
+import copy
+
+import pytest
+import torch
+
+from paper_2505_24034_amd import binding as L
+from paper_2505_24034_amd.optim import AdamW
+
+
+def _params(dtype=torch.float32):
+    g = torch.Generator().manual_seed(1)
+    return [torch.nn.Parameter(torch.randn(s, generator=g).to(dtype)) for s in ((3, 5), (7,))]
+
+
+def _saved(cls=torch.optim.AdamW, dtype=torch.float32, steps=2, **kw):
+    """the state_dict of one of torch's optimisers after some steps"""
+    ps = _params(dtype)
+    opt = cls(ps, lr=1e-2, **kw)
+    for _ in range(steps):
+        for p in ps:
+            p.grad = torch.ones_like(p)
+        opt.step()
+    return opt.state_dict()
+
+
+@pytest.mark.parametrize("cls,kw,names", [(torch.optim.AdamW, dict(maximize=True), ["maximize"]), (torch.optim.AdamW, dict(amsgrad=True), ["amsgrad"]),
+                                          (torch.optim.AdamW, dict(amsgrad=True, maximize=True), ["amsgrad", "maximize"]),
+                                          (torch.optim.Adam, dict(weight_decay=0.1), ["decoupled_weight_decay"])])
+def test_settings_that_are_not_followed_are_refused(cls, kw, names):
+    opt = AdamW(_params(), lr=1e-3)
+    before = copy.deepcopy(opt.state_dict())
+    with pytest.raises(L.LlamarlError) as e:
+        opt.load_state_dict(_saved(cls, **kw))
+    assert all(n in str(e.value) for n in names)
+    assert opt.state_dict() == before                                      # nothing was taken
+    if cls is torch.optim.AdamW:                                           # nor through a group's own settings
+        with pytest.raises(L.LlamarlError):
+            AdamW([dict(params=_params(), **kw)], lr=1e-3)
+
+
+@pytest.mark.parametrize("cls,kw", [(torch.optim.AdamW, dict(weight_decay=0.1)), (torch.optim.Adam, dict())])
+def test_settings_that_are_followed_are_taken(cls, kw):
+    opt = AdamW(_params(), lr=1e-3)
+    saved = _saved(cls, betas=(0.8, 0.9), eps=1e-6, **kw)
+    opt.load_state_dict(saved)
+    g = opt.param_groups[0]
+    assert (g["lr"], g["betas"], g["eps"], g["weight_decay"]) == (1e-2, (0.8, 0.9), 1e-6, kw.get("weight_decay", 0))
+    for i, p in enumerate(g["params"]):
+        s = opt.state[p]
+        assert s["step"] == 2 and isinstance(s["step"], int)
+        for name in ("exp_avg", "exp_avg_sq"):
+            assert torch.equal(s[name], saved["state"][i][name]) and s[name].data_ptr() != saved["state"][i][name].data_ptr()
