@@ -101,9 +101,22 @@ class AdamW(torch.optim.Optimizer):
 
     def load_state_dict(self, state_dict):
         """As torch's, which would turn the states into the parameters' type.  float32 states of torch.optim.AdamW can be gone on from."""
-        for group in state_dict["param_groups"]:
-            self._check_group(group)
-        super().load_state_dict(state_dict)
+        seen = []                                         # what torch takes: its hooks may have made another one of state_dict
+
+        def check(_, taken):
+            for group in taken["param_groups"]:
+                self._check_group(group)
+            seen.append(taken)
+
+        handles = [self.register_load_state_dict_pre_hook(check),                                    # behind all others
+                   self.register_load_state_dict_post_hook(lambda _: self._take(seen[0]), prepend=True)]      # ahead of them
+        try:
+            super().load_state_dict(state_dict)
+        finally:
+            for h in handles:
+                h.remove()
+
+    def _take(self, state_dict):
         saved = [k for group in state_dict["param_groups"] for k in group["params"]]
         for k, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
             if k in state_dict["state"]:

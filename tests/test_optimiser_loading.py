@@ -51,3 +51,37 @@ def test_settings_that_are_followed_are_taken(cls, kw):
         assert s["step"] == 2 and isinstance(s["step"], int)
         for name in ("exp_avg", "exp_avg_sq"):
             assert torch.equal(s[name], saved["state"][i][name]) and s[name].data_ptr() != saved["state"][i][name].data_ptr()
+
+
+def test_hooks_of_a_load_see_and_change_what_is_taken():
+    """the dict that a hook before the load returns is the one that is taken, and a hook behind it finds the states in place"""
+    saved = _saved()
+    renamed = dict(saved, state={i + 1: s for i, s in saved["state"].items()}, param_groups=[dict(saved["param_groups"][0], params=[1, 2])])
+    untouched = copy.deepcopy(renamed)
+    opt = AdamW(_params(), lr=1e-3)
+
+    def before(o, d):
+        assert o is opt
+        return dict(d, state={k: dict(s, exp_avg=s["exp_avg"] * 2, step=7) for k, s in d["state"].items()})
+
+    def behind(o):
+        for s in o.state.values():
+            assert s["step"] == 7 and isinstance(s["step"], int)
+            s["exp_avg"] += 1
+
+    opt.register_load_state_dict_pre_hook(before)
+    opt.register_load_state_dict_post_hook(behind)
+    for _ in range(2):                                                     # a load leaves no hook of its own behind
+        opt.load_state_dict(renamed)
+        for i, p in enumerate(opt.param_groups[0]["params"]):
+            assert torch.equal(opt.state[p]["exp_avg"], saved["state"][i]["exp_avg"] * 2 + 1)
+    for i in (1, 2):
+        assert torch.equal(renamed["state"][i]["exp_avg"], untouched["state"][i]["exp_avg"])
+
+
+def test_settings_that_a_hook_brings_are_looked_at():
+    opt = AdamW(_params(), lr=1e-3)
+    opt.register_load_state_dict_pre_hook(lambda o, d: dict(d, param_groups=[dict(g, maximize=True) for g in d["param_groups"]]))
+    with pytest.raises(L.LlamarlError):
+        opt.load_state_dict(_saved())
+    assert not opt.state
