@@ -11,8 +11,8 @@ class AdamW(torch.optim.Optimizer):
 
     state_bits      32, or 8: a quarter of the memory (binding.adamw_step says how they are held)
     master_weights  keep a float32 copy of bfloat16 parameters, which is what moves; without it changes below half a
-                    parameter's last bit are lost.  It is taken at the parameter's first step: weights that are loaded later have to
-                    come with the optimiser's state
+                    parameter's last bit are lost.  It is taken at the parameter's first step, or the first behind a load of states
+                    without one: weights that are loaded later have to come with the optimiser's state
     max_grad_norm   scale the gradients of all groups down to this norm; `grad_norm` then holds the norm before it (one
                     element, on the device).  A norm that is not finite leaves every parameter and state as it was (the step is
                     counted); without max_grad_norm nothing looks for such gradients
@@ -57,9 +57,10 @@ class AdamW(torch.optim.Optimizer):
         else:
             for name in ("exp_avg", "exp_avg_sq"):
                 s[name] = torch.zeros(p.shape, device=p.device)
-        if self.master_weights and p.dtype == torch.bfloat16:
-            s["master"] = p.detach().float()
         return s
+
+    def _has_master(self, p):
+        return self.master_weights and p.dtype == torch.bfloat16
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -79,6 +80,8 @@ class AdamW(torch.optim.Optimizer):
                 if p.grad.is_sparse:
                     raise L.LlamarlError(L.ERR_UNSUPPORTED, "sparse gradients")
                 s = self.state[p] if self.state[p] else self._init_state(p)
+                if self._has_master(p) and "master" not in s:
+                    s["master"] = p.detach().float()
                 runs.setdefault((i, s["step"] + 1), []).append((p, p.grad.contiguous()))
         if not runs:
             return loss
@@ -100,12 +103,17 @@ class AdamW(torch.optim.Optimizer):
         return loss
 
     def load_state_dict(self, state_dict):
-        """As torch's, which would turn the states into the parameters' type.  float32 states of torch.optim.AdamW can be gone on from."""
+        """As torch's, which would turn the states into the parameters' type.  float32 states of torch.optim.AdamW can be gone on from
+        with state_bits=32; states of another type than state_bits asks for are refused.  Master copies are taken where this
+        optimiser keeps them."""
         seen = []                                         # what torch takes: its hooks may have made another one of state_dict
 
         def check(_, taken):
             for group in taken["param_groups"]:
                 self._check_group(group)
+            for k, p in self._saved_places(taken):
+                if taken["state"].get(k):
+                    self._check_state(p, taken["state"][k])
             seen.append(taken)
 
         handles = [self.register_load_state_dict_pre_hook(check),                                    # behind all others
@@ -116,9 +124,25 @@ class AdamW(torch.optim.Optimizer):
             for h in handles:
                 h.remove()
 
-    def _take(self, state_dict):
+    def _saved_places(self, state_dict):
+        """(key of a saved state, parameter)"""
         saved = [k for group in state_dict["param_groups"] for k in group["params"]]
-        for k, p in zip(saved, [p for group in self.param_groups for p in group["params"]]):
+        return zip(saved, [p for group in self.param_groups for p in group["params"]])
+
+    def _check_state(self, p, s):
+        want = dict.fromkeys(("exp_avg", "exp_avg_sq"), (torch.float8_e4m3fn if self.state_bits == 8 else torch.float32, p.numel()))
+        if self.state_bits == 8:
+            want.update(dict.fromkeys(("exp_avg_scale", "exp_avg_sq_scale"), (torch.float32, -(-p.numel() // L.STATE_BLOCK))))
+        if self._has_master(p) and "master" in s:
+            want["master"] = (torch.float32, p.numel())
+        for name, (dtype, n) in want.items():
+            x = s.get(name)
+            if not torch.is_tensor(x) or x.dtype != dtype or x.numel() != n:
+                raise L.LlamarlError(L.ERR_INVALID_ARG, "saved states with %s of %s; state_bits=%d takes %d entries of %s here" % (
+                    name, "%d entries of %s" % (x.numel(), x.dtype) if torch.is_tensor(x) else type(x).__name__, self.state_bits, n, dtype))
+
+    def _take(self, state_dict):
+        for k, p in self._saved_places(state_dict):
             if k in state_dict["state"]:
                 self.state[p] = {name: int(v) if name == "step" else v.detach().to(p.device, copy=True) if torch.is_tensor(v) else v
-                                 for name, v in state_dict["state"][k].items()}
+                                 for name, v in state_dict["state"][k].items() if name != "master" or self._has_master(p)}

@@ -85,3 +85,63 @@ def test_settings_that_a_hook_brings_are_looked_at():
     with pytest.raises(L.LlamarlError):
         opt.load_state_dict(_saved())
     assert not opt.state
+
+
+def _own(bits, dtype, master):
+    """(optimiser, its state as a step would have left it) without a step"""
+    opt = AdamW(_params(dtype), lr=1e-3, state_bits=bits, master_weights=master)
+    for p in opt.param_groups[0]["params"]:
+        s = opt._init_state(p)
+        s["step"] = 3
+        if master and dtype == torch.bfloat16:
+            s["master"] = p.detach().float() + 2.0 ** -12
+    return opt
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_of_other_bits_are_refused(bits):
+    opt = AdamW(_params(), lr=1e-3, state_bits=bits)
+    with pytest.raises(L.LlamarlError, match="state_bits=%d" % bits):
+        opt.load_state_dict(_own(40 - bits, torch.float32, True).state_dict())
+    assert not opt.state
+    if bits == 8:                                                          # torch's own are in 32 bits
+        with pytest.raises(L.LlamarlError, match="state_bits=8"):
+            opt.load_state_dict(_saved())
+    for drop in ("exp_avg", "exp_avg_sq") + (("exp_avg_scale", "exp_avg_sq_scale") if bits == 8 else ()):
+        saved = _own(bits, torch.float32, True).state_dict()
+        for s in saved["state"].values():
+            s[drop] = s[drop].view(torch.uint8)[:2].view(s[drop].dtype) if s[drop].dtype == torch.float8_e4m3fn else s[drop].reshape(-1)[:0]
+        with pytest.raises(L.LlamarlError, match=drop):
+            opt.load_state_dict(saved)
+    with pytest.raises(L.LlamarlError, match="bfloat16"):                  # torch keeps bf16 parameters' states in bf16
+        AdamW(_params(torch.bfloat16), lr=1e-3).load_state_dict(_saved(dtype=torch.bfloat16))
+    opt.load_state_dict(_own(bits, torch.float32, True).state_dict())
+    assert all(s["step"] == 3 for s in opt.state.values())
+
+
+def test_master_copies_are_there_where_they_are_asked_for(monkeypatch):
+    calls = []
+    monkeypatch.setattr(L, "adamw_step", lambda params, *a, **kw: calls.append((params, kw["masters"])))
+    for saved_master in (True, False):
+        for master in (True, False):
+            saved = _own(32, torch.bfloat16, saved_master).state_dict()
+            opt = AdamW(_params(torch.bfloat16), lr=1e-3, master_weights=master)
+            opt.load_state_dict(saved)
+            ps = opt.param_groups[0]["params"]
+            with torch.no_grad():
+                for p in ps:
+                    p += 1                                                 # weights that are loaded behind the states
+                    p.grad = torch.ones_like(p)
+            opt.step()
+            params, masters = calls.pop()
+            assert all(a is b for a, b in zip(params, ps))
+            for i, (p, m) in enumerate(zip(ps, masters)):
+                if not master:
+                    assert m is None
+                elif saved_master:
+                    assert torch.equal(m, saved["state"][i]["master"]) and m.data_ptr() != saved["state"][i]["master"].data_ptr()
+                else:
+                    assert m.dtype == torch.float32 and torch.equal(m, p.detach().float())
+    opt = AdamW(_params(torch.float32), lr=1e-3)                           # float32 parameters have none
+    opt.load_state_dict(_own(32, torch.bfloat16, True).state_dict())
+    assert all("master" not in s for s in opt.state.values())
