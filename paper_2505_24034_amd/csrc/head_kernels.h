@@ -506,7 +506,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a, Targe
         if (m > M) {
           S = S * __expf(M - m) + s;      // exp(-inf) = 0 on the first tile
           M = m;
-        } else if (m != -INFINITY) {
+        } else if (s != 0.f) {            // 0: a tile of -inf alone.  One of NaN alone has m = -inf too, and s = NaN
           S += s * __expf(m - M);
         }
       }
@@ -551,7 +551,7 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a, Targe
     for (int q = 1; q < WAVES; ++q) Mx = fmaxf(Mx, s_M[q][tok]);
     float Sx = 0.f;
 #pragma unroll
-    for (int q = 0; q < WAVES; ++q) Sx += (s_M[q][tok] == -INFINITY) ? 0.f : s_S[q][tok] * expf(s_M[q][tok] - Mx);
+    for (int q = 0; q < WAVES; ++q) Sx += (s_S[q][tok] == 0.f) ? 0.f : s_S[q][tok] * expf(s_M[q][tok] - Mx);
     const int64_t t = a.rows[p];
     if constexpr (PARTIAL) {
       const int64_t y = (int64_t)a.targets[t] - a.v_off;
@@ -569,21 +569,20 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a, Targe
 
 // The all-reduce of a vocabulary-parallel head, done here for shards that ran one after another on one GPU:
 //   M = max_p m_p,  lse = M + log sum_p s_p exp(m_p - M),  logp = sum_p zt_p - lse        (m, s, zt: [shards][N])
-// Rows whose every m_p is -inf (masked / bad target in every shard) get logp = lse = 0.  Shards are summed in
-// ascending order: deterministic.
+// Rows whose every m_p is -inf (masked / bad target in every shard) get logp = lse = 0, but for those with a logit that is NaN.  Shards
+// are summed in ascending order: deterministic.
 __global__ __launch_bounds__(256) void k_merge_shards(const float* m, const float* s, const float* zt, int shards,
                                                        int64_t N, float* logp, float* lse) {
   for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < N; t += (int64_t)gridDim.x * 256) {
     float M = -INFINITY;
     for (int p = 0; p < shards; ++p) M = fmaxf(M, m[(int64_t)p * N + t]);
-    float l = 0.f, lp = 0.f;
-    if (M != -INFINITY) {
-      float S = 0.f, Z = 0.f;
-      for (int p = 0; p < shards; ++p) {
-        const float mp = m[(int64_t)p * N + t];
-        S += (mp == -INFINITY) ? 0.f : s[(int64_t)p * N + t] * expf(mp - M);
-        Z += zt[(int64_t)p * N + t];
-      }
+    float l = 0.f, lp = 0.f, S = 0.f, Z = 0.f;
+    for (int p = 0; p < shards; ++p) {
+      const float mp = m[(int64_t)p * N + t], sp = s[(int64_t)p * N + t];
+      S += (mp == -INFINITY && !isnan(sp)) ? 0.f : sp * expf(mp - M);      // s is NaN where a logit is, whatever m says
+      Z += zt[(int64_t)p * N + t];
+    }
+    if (M != -INFINITY || isnan(S)) {
       l = M + logf(S);
       lp = Z - l;
     }
