@@ -470,12 +470,13 @@ struct MergeArgs {
   float* out0;            // full vocabulary: logp           shard: m   (max of the shard's logits)
   float* out1;            //                  lse                   s   (sum of exp(z - m) over the shard)
   float* out2;            //                  unused                zt  (target logit if the shard owns it, else 0)
-  const int32_t* targets; // shard only
+  const int32_t* targets; // shard, and targets that are formed again
   int64_t v_off, V;       // shard only: its vocabulary range is [v_off, v_off + V)
 };
 // PARTIAL: W is a shard of a vocabulary-parallel head; the per-token (m, s, zt) are what the shards would
 // all-reduce (paper Sec. 8.2, Table 3: trainer model parallelism 8-32), see k_merge_shards.
-// Target: forms the target logits of the block's tokens again (block_kernels.h), in place of zt.
+// Target: forms the target logits of the block's tokens again (block_kernels.h), more precisely than the tiles did.  Its term of
+// the sum is replaced too: a token that has nearly all of the probability would otherwise leave the difference of the two logits in logp.
 struct StoredTarget {
   static constexpr bool FORMED = false;
 };
@@ -560,9 +561,16 @@ __global__ __launch_bounds__(MERGE_THREADS) void k_merge_logp(MergeArgs a, Targe
       a.out2[t] = (y >= 0 && y < a.V) ? a.zt[p] : 0.f;
     } else {
       // in double: lse and logp each carry one fp32 rounding, at the size of the result
-      const double l = (double)Mx + log((double)Sx);
-      a.out1[t] = (float)l;
-      a.out0[t] = (float)((double)(Target::FORMED ? s_z[tok] : a.zt[p]) - l);
+      if constexpr (Target::FORMED) {
+        const double z = s_z[tok], term = exp(z - (double)Mx), rest = (double)Sx - exp((double)a.zt[p] - (double)Mx);
+        const double l = (double)Mx + log((rest < 0.0 ? 0.0 : rest) + term);      // rest: fp32 sums, a last bit below 0 at most
+        a.out1[t] = (float)l;
+        a.out0[t] = z > l ? 0.f : (float)(z - l);
+      } else {
+        const double l = (double)Mx + log((double)Sx);
+        a.out1[t] = (float)l;
+        a.out0[t] = (float)((double)a.zt[p] - l);
+      }
     }
   }
 }
