@@ -417,8 +417,8 @@ llamarl_status llamarl_quantise_blocks(const void* x, int64_t rows, int64_t cols
  *   H, H_scale  in  [N,d], d % 16 == 0, block_rows = 1;  N * d < 2^31
  *   W, W_scale  in  [V,d], block_rows = 128;  V < 2^21
  *   z           out [N,V] of type z_dt; apart from the operands
- * A scale byte is 0 .. 254; two whose product exceeds 2^127 count as 2^127 in fp32 sums.  fp32 logits, and all of up to 64 tokens and
- * 32640 rows, are fp32 sums of exact products.  bf16 logits of more come from the 8-bit matrix instructions, which add eight products
+ * A scale byte is 0 .. 254; two whose product exceeds 2^127 count as 2^127 in fp32 sums.  fp32 logits, and all of up to 64
+ * tokens, are fp32 sums of exact products.  bf16 logits of more come from the 8-bit matrix instructions, which add eight products
  * at a time and cut each at 2^-13 of the largest: less than 2^-10 of the sum of a logit's terms' magnitudes and, where their signs are
  * random, 1.5e-5 of the root of their sum of squares (measured).
  */

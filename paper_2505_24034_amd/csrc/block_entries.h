@@ -142,6 +142,7 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   BlockLogitsArgs a = {};
   a.x = x; a.N = N; a.d = d; a.V = V; a.z = z; a.v_end = plan.rows;
   if (z_dt == LLAMARL_F32) return (plan.tile == BLOCK_64 ? launch_block_logits<Exact64, float> : launch_block_logits<Exact128, float>)(a, st);
+  if (N <= FEW_TOKENS) return (plan.tile == BLOCK_64 ? launch_block_logits<Exact64, uint16_t> : launch_block_logits<Exact128, uint16_t>)(a, st);
   const auto launch = [&](BlockTile t) {
     return (t == BLOCK_256   ? launch_block_logits<Blocks256, uint16_t>
             : t == BLOCK_128 ? launch_block_logits<Blocks128, uint16_t>
@@ -190,17 +191,20 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
   k_compact_rows<<<dim3((unsigned)compact_blocks(N)), dim3(COMPACT_THREADS), 0, st>>>(
       compact_args({0, mask, targets, nullptr, V, N, 0, rows, n_act, logp, lse, nullptr, 0.f, nullptr, nullptr}));
   HIP_TRY(hipGetLastError());
+  const bool exact = N <= FEW_TOKENS;
   if (tile <= BLOCK_FEW) {
     FewArgs f = {};
     f.x = x; f.N = N; f.d = d; f.V = V; f.f = a;
     s = launch_few<void>(f, tile, st);
+  } else if (exact) {
+    s = (tile == BLOCK_64 ? launch_block_partials<Exact64> : launch_block_partials<Exact128>)(a, x, st);
   } else {
     s = (tile == BLOCK_256   ? launch_block_partials<Blocks256>
          : tile == BLOCK_128 ? launch_block_partials<Blocks128>
                              : launch_block_partials<Blocks64>)(a, x, st);
   }
   if (s != LLAMARL_OK) return s;
-  if (tile <= BLOCK_FEW) return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);
+  if (exact) return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);
   return launch_merge(a, logp, lse, nullptr, 0, BlockTarget{x, N, V, (int)d}, st);
 }
 

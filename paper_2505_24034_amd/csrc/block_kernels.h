@@ -3,7 +3,7 @@
 //   k_quantise_rows, k_quantise_tiles   e4m3 and a power of two for each 1 x 128 (activations) or 128 x 128 (weights) block
 //   k_block_logits     z = H W^T of two such matrices, stored
 //   k_block_partials   the same tiles reduced to (max, sum of exp, target logit) a token: token_logprobs without logits in memory
-//   k_few_direct, k_few_tokens   both for up to 16 and 64 tokens, bound by the bytes of W
+//   k_few_direct, k_few_tokens   both for up to 16 and 64 tokens and few rows, bound by the bytes of W
 //
 // A block's scale 2^e is the smallest power of two for which no finite entry exceeds 448 * 2^e, held as the byte e + 127;
 // q = x / 2^e is exact before it is rounded to e4m3, and so are the products with the scales.  Entries that are not finite become NaN.

@@ -273,11 +273,14 @@ constexpr int DIRECT_WAVES = 8, FEW_ROWS = 64;
 //   (8, 128256, 256)         10.5 / 32 / 13.5                                10.7,  24 : 32
 // (tiles of 128 x 128).  So tiles where there is one of those for every CU, though most such calls then take 64 x 64 ones (below), else the
 // direct kernel for up to four tokens and for few rows, the one through LDS to 64 tokens.
+// All of up to 64 tokens are sums in fp32, tiles' too (TileGemmBlocksSimple, EXACT).  Tiles on the 8-bit pipe : fp32, us: bf16 logits
+// (6, 33001, 2048) 17.5 : 18.6, (33, 33001, 2048) 18.8 : 21.8, (33, 66000, 4096) 69 : 69, (1, 128256, 4096) 97 : 98, (64, 128256, 4096) 113 : 115;
+// log-probs 27.4 : 27.3, 28.3 : 30.4, 82 : 80, 113 : 114, 115 : 118.  So W's bytes are the time on either, and the sums are better.
 enum BlockTile { BLOCK_DIRECT, BLOCK_FEW, BLOCK_64, BLOCK_128, BLOCK_256 };
 // Fewer tiles of 128 x 128 than this are cut into 64 x 64.  us at (N, V, d), 128 / 64, fp32 | bf16: (100, 4346, 1104) 18 / 9.0 | 9.9 / 6.5,
 // (200, 1000, 4096) 48 / 21 | 20 / 13, (100, 16032, 8192) 85 / 52 | 45 / 35, (300, 8000, 1024) 18.3 / 14.5 | 10.7 / 10.2 (log-probs 16.9 / 18.2),
 // (128, 33001, 4096) 67 / 53 | 36 / 39, (1041, 5003, 528) 18.6 / 22.3 | 13.4 / 19.1
-// FEW: with up to 64 tokens, whose tiles wait for W, four small ones on a CU ask for as much and are spread more evenly.  bf16 | fp32
+// FEW: with up to 64 tokens, whose tiles wait for W, four small ones on a CU ask for as much and are spread more evenly.  bf16 (8-bit pipe) | fp32
 // logits, 128 / 64: (43, 44347, 4688) 75 / 67 (log-probs 84 / 75), (64, 33001, 2048) 23.7 / 20.1, (20, 66000, 4096) 89 / 75 | 96 / 77, (30, 70000, 4096)
 // 91 / 82 | 102 / 87, (1, 40000, 8192) 95 / 64 (102 / 72), (1, 128256, 4096) 108 / 105 | 108 / 103; (48, 128256, 4096) 117 / 117 | 118 / 129,
 // (64, 128256, 8192) 217 / 228 | 223 / 244.  fp32, kernels for few tokens / 64 x 64: (10, 16032, 4096) 17 / 25, (48, 24000, 4096) 37 / 38, (3, 33001, 2048)
@@ -291,7 +294,8 @@ LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
   // 153 : 194, (1024, ..) 524 : 667
   return !exact && N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
 }
-// bf16 logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own.
+// bf16 logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own
+// (more than 64 tokens).
 struct BlockLogits {
   BlockTile tile;
   int64_t rows;
@@ -308,7 +312,7 @@ LLAMARL_RULE int64_t block_cost_128(int64_t N, int64_t V, int64_t d) {
 }
 LLAMARL_RULE BlockLogits block_logits(int64_t N, int64_t V, int64_t d) {
   const BlockTile t = block_tile(N, V, false);
-  if (t < BLOCK_128) return {t, V, t};
+  if (N <= FEW_TOKENS || t < BLOCK_128) return {t, V, t};
   const int64_t tiles_t = (N + 255) / 256, tiles = tile_count(N, V, 256), rows = tiles / 256 * 256 / tiles_t * 256;
   const int64_t round = (14000 + 25 * d / 2) * (4 * tiles_t - ((N - 1) % 256 < 128)) / (4 * tiles_t);
   BlockLogits best = {BLOCK_128, V, BLOCK_128};
