@@ -132,7 +132,7 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
                   {{H, N * d}, {H_scale, groups * N * 4}, {W, V * d}, {W_scale, groups * ((V + SCALE_BLOCK - 1) / SCALE_BLOCK) * 4}}))
     return fail(LLAMARL_ERR_INVALID_ARG, "z must not overlap an operand");
   const BlockHead x = block_head(H, H_scale, W, W_scale);
-  const BlockLogits plan = z_dt == LLAMARL_F32 ? BlockLogits{block_tile(N, V, true), V, BLOCK_64} : block_logits(N, V, d);
+  const BlockLogits plan = z_dt == LLAMARL_F32 && N > FEW_TOKENS ? BlockLogits{block_tile(N, V, true), V, BLOCK_64} : block_logits(N, V, d);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   if (plan.tile <= BLOCK_FEW) {
     FewArgs f = {};

@@ -294,8 +294,24 @@ LLAMARL_RULE BlockTile block_tile(int64_t N, int64_t V, bool exact) {
   // 153 : 194, (1024, ..) 524 : 667
   return !exact && N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? BLOCK_256 : BLOCK_128;
 }
+// wavefronts of k_few_direct that share rows of W: as many as have a group (512 columns) of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192)
+// 51 / 32 / 32 / 29, (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23
+LLAMARL_RULE int direct_parts(int64_t d) {
+  const int64_t groups = (d + 511) / 512;
+  return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
+}
+// Logits of one or two tokens on a little more than 32640 rows, whose 64 x 64 tiles are about half of the four that a CU takes: the direct kernel, where
+// all of its wavefronts have as many groups of K.  Tiles / direct, fp32 logits of 1 | 2 tokens, us: (32900, 4096) 35.6 / 29.3 | 35.6 / 30.8, (36000, 2048)
+// 19.5 / 18.0 | 19.5 / 18.5, (39000, 4096) 36.3 / 33.2 | 36.5 / 35.2, (41000, 8192) 64.7 / 66.2 | 64.9 / 68.8, (44000, 2048) 20.6 / 20.8 | 20.6 / 21.5;
+// groups that do not divide (33001, 1536) 15.2 / 16.8 (though (36000, 6144) 50.7 / 45.8), one group (33001, 512) 7.9 / 8.4; three tokens (44000, 4096) 37.8 / 39.9.  Log-probs, whose direct
+// tiles are of 16 rows: (33001, 8192) 67 / 73.
+constexpr int64_t DIRECT_LOGITS_TILES = 640;
+LLAMARL_RULE bool direct_logits(int64_t N, int64_t V, int64_t d) {
+  const int64_t groups = (d + 511) / 512;
+  return N <= 2 && (V + 63) / 64 <= DIRECT_LOGITS_TILES && groups >= 2 && groups % direct_parts(d) == 0;
+}
 // bf16 logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own
-// (more than 64 tokens).
+// (more than 64 tokens; up to those it is fp32 logits' rule too).
 struct BlockLogits {
   BlockTile tile;
   int64_t rows;
@@ -311,7 +327,7 @@ LLAMARL_RULE int64_t block_cost_128(int64_t N, int64_t V, int64_t d) {
   return tiles <= 256 ? round * 2 / 3 : (tiles + 511) / 512 * round;
 }
 LLAMARL_RULE BlockLogits block_logits(int64_t N, int64_t V, int64_t d) {
-  const BlockTile t = block_tile(N, V, false);
+  const BlockTile t = direct_logits(N, V, d) ? BLOCK_DIRECT : block_tile(N, V, false);
   if (N <= FEW_TOKENS || t < BLOCK_128) return {t, V, t};
   const int64_t tiles_t = (N + 255) / 256, tiles = tile_count(N, V, 256), rows = tiles / 256 * 256 / tiles_t * 256;
   const int64_t round = (14000 + 25 * d / 2) * (4 * tiles_t - ((N - 1) % 256 < 128)) / (4 * tiles_t);
@@ -325,12 +341,6 @@ LLAMARL_RULE BlockLogits block_logits(int64_t N, int64_t V, int64_t d) {
   if (rows > 0 && rows < V && tiles / 256 * round + block_cost_128(N, V - rows, d) + 3000 < cost)
     best = {BLOCK_256, rows, tile_count(N, V - rows, 128) < BLOCK_64_TILES ? BLOCK_64 : BLOCK_128};
   return best;
-}
-// wavefronts of k_few_direct that share rows of W: as many as have a group (512 columns) of K.  1 / 2 / 4 / 8 of them, us: (1, 16032, 8192)
-// 51 / 32 / 32 / 29, (8, 1000, 8192) 48 / 26 / 15 / 8.8, (1, 33001, 2048) 22 / 17 / 15 / 15, (8, 128256, 256) 10 / 11 / 15 / 23
-LLAMARL_RULE int direct_parts(int64_t d) {
-  const int64_t groups = (d + 511) / 512;
-  return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
 }
 // rows of W that a tile of partials has
 LLAMARL_RULE int block_tile_rows(BlockTile t, int64_t d) {

@@ -36,3 +36,24 @@ def test_sums_in_fp32(lib, N, d, V, kernel):
     last = 16 * U * (np.abs(want_lse) + np.abs(want_logp) + 8)
     assert (np.abs(lse - want_lse) <= off + last).all()
     assert (np.abs(logp - want_logp) <= 2 * off + last).all()
+
+
+@pytest.mark.parametrize("N,V,d", [(1, 32641, 1040), (2, 40960, 1024), (1, 40945, 2048), (2, 34567, 4096)])
+def test_one_or_two_tokens_straight_from_memory(lib, N, V, d):
+    """the logits' kernel without LDS beside the log-probabilities' tiles"""
+    assert lib._load_native().block_plan(N, V, d, 0)[0] == 2
+    g = torch.Generator(device="cuda").manual_seed(V)
+    H, W = torch.randn(N, d, generator=g, device="cuda"), torch.randn(V, d, generator=g, device="cuda") * d ** -0.5
+    x = (*lib.quantise_blocks(H, 1), *lib.quantise_blocks(W, 128))
+    out = torch.full((N + 2, V), 7.0, device="cuda").view(-1)
+    off = -V % 4                                                           # 16-byte aligned rows behind the first
+    z = lib.logits_blocks(*x, out=out[V + off:V + off + N * V].view(N, V))
+    assert (out[:V + off] == 7).all() and (out[V + off + N * V:] == 7).all()
+    Hd, Wd = (torch.from_numpy(dequantise(q, s, b)).cuda() for q, s, b in ((x[0], x[1], 1), (x[2], x[3], 128)))
+    want, rss = Hd @ Wd.T, torch.sqrt((Hd * Hd) @ (Wd * Wd).T)
+    assert ((z.double() - want).abs() <= 4 * (d ** 0.5 + 4) * U * rss + U * want.abs()).all()
+    assert torch.equal(lib.logits_blocks(*x, dtype=torch.bfloat16), z.to(torch.bfloat16))
+    t = torch.randint(0, V, (N,), generator=g, device="cuda").int()
+    lse = lib.token_logprobs_blocks(*x, t)[1]
+    ref = torch.logsumexp(want, 1)
+    assert ((lse - ref).abs() <= 4 * (d ** 0.5 + 4) * U * rss.amax(dim=1) + 16 * U * (2 * ref.abs() + 20)).all()
