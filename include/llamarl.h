@@ -365,15 +365,18 @@ llamarl_status llamarl_grad_norm(const llamarl_gradient* grads, int64_t count, f
  * each kind, and
  *     m = m_scale[b] * e4m3(m[i])        sqrt(v) = v_scale[b] * e4m3(v[i])
  * with factor = (largest magnitude of the block) / 448 after the step, 0 for a block below 2^-100.  p moves by the states
- * before they are rounded.  m is rounded to nearest.  sqrt(v) changes by less than a rounding step in an update and is
- * rounded up or down by 16 bits hashed out of (step, place in the list, entry), so that its mean is right; a v that is not zero
- * is not rounded to zero.  Zero bytes and factors are the states of a fresh tensor.  A gradient that is not finite (and no
- * grad_scale that says so) leaves NaN in its entry's parameter and states, an infinite one in its block's.
+ * before they are rounded.  m is rounded to nearest: it stays where it is while (1 - beta1) |g - m| is below half a step, which is
+ * |m| / 32 to |m| / 16, and m_scale / 1024 for entries up to m_scale / 64.  It so may end up to 0.63 |m| from a constant gradient with
+ * beta1 = 0.9; a larger beta1 than 15/16, at which an m would not even leave its place for a gradient of the other sign, is refused
+ * (INVALID_ARG).  sqrt(v) changes by less than a rounding step in an update and is rounded up or down by 16 bits hashed out of (step,
+ * place in the list, entry), so that its mean is right; a v that is not zero is not rounded to zero, and below v_scale / 512 counts as
+ * that.  Zero bytes and factors are the states of a fresh tensor.  A gradient that is not finite (and no grad_scale that says so)
+ * leaves NaN in its entry's parameter and states, an infinite one, or one whose square is beyond fp32, in its block's.
  *
  *   tensors      HOST array [count]; its arrays are on the device.  Tensors of any mixture of types; empty ones (n = 0) take no
  *                part.  Arrays need the alignment of their type only (16-byte aligned ones are faster); nothing that is written
  *                may overlap another array of the call (INVALID_ARG).
- *   p            HOST pointer; lr, eps, weight_decay >= 0, betas in [0, 1), step >= 1
+ *   p            HOST pointer; lr, eps, weight_decay >= 0, betas in [0, 1) (beta1 <= 15/16 with states in 8 bits), step >= 1
  *   grad_scale   device float [1] or NULL (= 1).  If it is not finite when the kernels run, no step is taken: nothing is written
  *   lr_device    device float [1] or NULL; read when the kernels run, instead of p->lr (not checked)
  *   step_device  device int64 [1] or NULL; the same for p->step (taken as 1 where it is less)

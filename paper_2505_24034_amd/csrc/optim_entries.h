@@ -134,6 +134,8 @@ llamarl_status check_adamw(const llamarl_adamw_tensor* tensors, int64_t count, c
     if (!t.param || !t.grad || !t.m || !t.v) return fail(LLAMARL_ERR_INVALID_ARG, "tensor %lld: null pointer", (long long)i);
     if ((t.m_scale == nullptr) != (t.v_scale == nullptr))
       return fail(LLAMARL_ERR_INVALID_ARG, "tensor %lld: both m_scale and v_scale, or neither", (long long)i);
+    if (t.m_scale != nullptr && p->beta1 > STATE_BETA1)
+      return fail(LLAMARL_ERR_INVALID_ARG, "tensor %lld: first moments in 8 bits need beta1 <= %g (got %g)", (long long)i, STATE_BETA1, p->beta1);
     if (t.master != nullptr && t.param_dt == LLAMARL_F32)
       return fail(LLAMARL_ERR_INVALID_ARG, "tensor %lld: a master copy of fp32 parameters", (long long)i);
     if (!aligned_to(t.param, esize(t.param_dt)) || !aligned_to(t.grad, esize(t.grad_dt)) || !aligned_to(t.master, 4) ||

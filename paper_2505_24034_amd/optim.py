@@ -9,7 +9,7 @@ from . import binding as L
 class AdamW(torch.optim.Optimizer):
     """params: contiguous float32 or bfloat16 tensors on the GPU, or groups of them.
 
-    state_bits      32, or 8: a quarter of the memory (binding.adamw_step says how they are held)
+    state_bits      32, or 8: a quarter of the memory (binding.adamw_step says how they are held); betas[0] is then 15/16 at most
     master_weights  keep a float32 copy of bfloat16 parameters, which is what moves; without it changes below half a
                     parameter's last bit are lost.  It is taken at the parameter's first step, or the first behind a load of states
                     without one: weights that are loaded later have to come with the optimiser's state
@@ -38,7 +38,10 @@ class AdamW(torch.optim.Optimizer):
         super().add_param_group(param_group)
 
     def _check_group(self, group):
-        """torch's settings that change the step and are not computed here"""
+        """torch's settings that change the step and are not computed here, and what states in 8 bits cannot follow"""
+        beta1 = group.get("betas", self.defaults["betas"])[0]
+        if self.state_bits == 8 and beta1 > L.STATE_BETA1:
+            raise L.LlamarlError(L.ERR_INVALID_ARG, "first moments in 8 bits need betas[0] <= %g (got %g)" % (L.STATE_BETA1, beta1))
         set_ = [name for name in ("amsgrad", "maximize") if group.get(name)]
         if not group.get("decoupled_weight_decay", True) and group.get("weight_decay", self.defaults["weight_decay"]):
             set_.append("decoupled_weight_decay=False")
@@ -73,6 +76,8 @@ class AdamW(torch.optim.Optimizer):
             raise L.LlamarlError(L.ERR_UNSUPPORTED, "a captured step would repeat its step count: capture binding.adamw_step "
                                                     "with step and lr on the device")
         runs = {}                                         # (group, step) -> parameters and gradients
+        for group in self.param_groups:                   # before any of them moves
+            self._check_group(group)
         for i, group in enumerate(self.param_groups):
             for p in group["params"]:
                 if p.grad is None:
