@@ -431,7 +431,7 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
 /*
  * llamarl_token_logprobs under such a head: the generator's mu of given tokens.  targets, mask, logp and lse as there; the logits
  * never reach memory.
- *   ws  scratch, >= llamarl_logprobs_blocks_workspace_bytes(N, V), which does not fall as N or V grows (0 for invalid sizes)
+ *   ws  scratch, >= llamarl_logprobs_blocks_workspace_bytes(N, V), which does not fall as N or V grows (0 for sizes that no d allows)
  * logp, lse and ws lie apart from each other and from the operands.  The target's logit and its term of the sum of exponentials are fp32
  * sums; the other terms come from the 8-bit instructions where bf16 logits do.  With p the target's probability, logp and lse are
  * then off by 1 - p times the mean of those logits' errors under the distribution: 1e-7 where it is flat (measured), one logit's

@@ -35,13 +35,14 @@ llamarl_status check_block_matrix(int64_t rows, int64_t cols) {
   if (cols >= (int64_t)1 << 22 || rows >= (int64_t)1 << 31) return fail(LLAMARL_ERR_UNSUPPORTED, "matrix too large");
   return LLAMARL_OK;
 }
+constexpr int64_t BLOCK_MOST_H = (int64_t)1 << 31, BLOCK_MOST_ROWS = (int64_t)1 << 21;      // N d and V of a head are below these
 llamarl_status check_block_head(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale, int64_t N, int64_t d, int64_t V) {
   if (!H || !H_scale || !W || !W_scale) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
   llamarl_status s = check_block_matrix(N, d);
   if (s == LLAMARL_OK) s = check_block_matrix(V, d);
   if (s != LLAMARL_OK) return s;
-  if (N * d >= (int64_t)1 << 31) return fail(LLAMARL_ERR_UNSUPPORTED, "H must be smaller than 2 GiB (its rows are gathered with 32-bit offsets)");
-  if (tile_count(N, V, 128) >= (int64_t)1 << 31 || V >= (int64_t)1 << 21) return fail(LLAMARL_ERR_UNSUPPORTED, "too many tiles or logits of a token");
+  if (N * d >= BLOCK_MOST_H) return fail(LLAMARL_ERR_UNSUPPORTED, "H must be smaller than 2 GiB (its rows are gathered with 32-bit offsets)");
+  if (tile_count(N, V, 128) >= (int64_t)1 << 31 || V >= BLOCK_MOST_ROWS) return fail(LLAMARL_ERR_UNSUPPORTED, "too many tiles or logits of a token");
   if (!aligned16(H) || !aligned16(W)) return fail(LLAMARL_ERR_INVALID_ARG, "H and W must be 16-byte aligned");
   if (!aligned_to(H_scale, 4) || !aligned_to(W_scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "scales must be 4-byte aligned");
   return LLAMARL_OK;
@@ -155,7 +156,9 @@ llamarl_status llamarl_logits_blocks(const void* H, const uint8_t* H_scale, cons
   return launch(plan.rest);
 }
 
-size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) { return N <= 0 || V <= 0 ? 0 : block_ws(N, V).total; }
+size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V) {
+  return N <= 0 || V <= 0 || N >= BLOCK_MOST_H / 16 || V >= BLOCK_MOST_ROWS ? 0 : block_ws(N, V).total;      // d >= 16
+}
 
 llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale,
                                              const int32_t* targets, const uint8_t* mask, int64_t N, int64_t d, int64_t V, float* logp,

@@ -21,3 +21,10 @@ def test_what_was_direct_stays_so():
         for V in (1, 1000, 16032, 32640):
             for d in (16, 512, 1536, 4096):
                 assert rules.block_logits_plan(N, V, d)[0] == rules.block_plan(N, V, d, 0)[0] == DIRECT
+
+
+def test_no_workspace_for_sizes_that_no_call_takes():
+    size = L.logprobs_blocks_workspace_bytes
+    for N, V in ((1, 1 << 21), (1 << 27, 5), (1 << 62, 1 << 62), (-1, 5), (5, -1)):
+        assert size(N, V) == 0, (N, V)
+    assert size((1 << 27) - 1, 5) >= size(1 << 20, 5) > 0 and size(5, (1 << 21) - 1) >= size(5, 1 << 20) > 0
