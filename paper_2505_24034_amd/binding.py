@@ -372,9 +372,10 @@ def adamw_step(params, grads, exp_avgs, exp_avg_sqs, lr, step, betas=(0.9, 0.999
                exp_avg_scales=None, exp_avg_sq_scales=None, grad_scale=None, stream=None):
     """llamarl_adamw_step: moves every tensor of `params` (float32 or bfloat16) and its states in place.  States are float32, or
     float8_e4m3fn with a float32 factor for each STATE_BLOCK entries in exp_avg_scales and exp_avg_sq_scales (exp_avg_sqs then
-    hold square roots, and betas[0] is STATE_BETA1 at most: exp_avgs are rounded to nearest and would stand still).  masters: float32 copies of bfloat16 parameters.  The last three lists may hold None for a
-    tensor.  lr and step may be one-element device tensors (float32, int64), read when the kernels run; grad_scale is one
-    (float32): where it is not finite, nothing is written."""
+    hold square roots, and betas[0] is STATE_BETA1 at most: exp_avgs are rounded to nearest and would stand still).  masters:
+    float32 copies of bfloat16 parameters.  The last three lists may hold None for a tensor.  lr and step may be one-element
+    device tensors (float32, int64), read when the kernels run; grad_scale is one (float32): where it is not finite, nothing is
+    written."""
     (_native or _load_native()).adamw_step(params, grads, exp_avgs, exp_avg_sqs, masters, exp_avg_scales, exp_avg_sq_scales, lr,
                                            betas[0], betas[1], eps, weight_decay, step, grad_scale, _handle(stream))
 

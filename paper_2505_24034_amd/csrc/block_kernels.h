@@ -313,11 +313,11 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_block_logit
 }
 
 // ---- the target's logit ------------------------------------------------------------------------------------------------------------
-// The 8-bit matrix pipe adds eight products at a time, each cut, towards zero, at 2^-13 of the largest of them (measured: beside 448 * 448,
-// terms below 8 vanish and 12 counts as 8, for seven of the 127 others): seven lose less than that each, so a logit is off by less than 2^-10 of the sum of its terms' magnitudes, and by
-// 1.5e-5 of the root of their sum of squares where their signs are random.  Over a flat distribution that averages out of the sum of exponentials (1e-7);
-// where one token has nearly all of it, it does not.  The target's logit, which enters a log-probability by itself, is formed again from its
-// widened entries, a wavefront a token, 2 d bytes, and so is its term of the sum (k_merge_logp).
+// The 8-bit matrix pipe adds eight products at a time, each cut, towards zero, at 2^-13 of the largest of them (measured: beside 448 * 448, terms
+// below 8 vanish and 12 counts as 8, for seven of the 127 others): seven lose less than that each, so a logit is off by less than 2^-10 of the sum of
+// its terms' magnitudes, and by 1.5e-5 of the root of their sum of squares where their signs are random.  Over a flat distribution that averages out
+// of the sum of exponentials (1e-7); where one token has nearly all of it, it does not.  The target's logit, which enters a log-probability by
+// itself, is formed again from its widened entries, a wavefront a token, 2 d bytes, and so is its term of the sum (k_merge_logp).
 __device__ __forceinline__ float e4m3_dot(uint32_t x, uint32_t y, float s) {
   const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)y, false);
   const auto c = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true), e = __builtin_amdgcn_cvt_pk_f32_fp8((int)y, true);
@@ -465,10 +465,10 @@ __global__ __launch_bounds__(FEW_THREADS, 4) void k_few_direct(FewArgs a) {
   }
 }
 
-// Up to 64 tokens.  A workgroup takes 64 rows of W: a wavefront 16 rows and one half of the groups; the halves meet in LDS at the end, in
-// order.  The tokens' part of a group is brought to LDS once for the four wavefronts of a half: read by each of them from L2 it was more
-// traffic than W's (48 tokens 217 - 250 us of a 128256 x 4096 head, 134 here).  W's registers are loaded again, for the next group, as soon as a
-// block is multiplied.  Workgroups start at groups of their own: see SlabOrder.
+// Up to 64 tokens.  A workgroup takes 64 rows of W: a wavefront 16 rows and one half of the groups; the halves meet in LDS at the end, in order.  The
+// tokens' part of a group is brought to LDS once for the four wavefronts of a half: read by each of them from L2 it was more traffic than W's (48
+// tokens of a 128256 x 4096 head, which takes tiles by now: 217 - 250 us, 134 here).  W's registers are loaded again, for the next group, as soon as
+// a block is multiplied.  Workgroups start at groups of their own: see SlabOrder.
 constexpr int FEW_PITCH = FEW_ROWS + 4;              // floats of a token's row in LDS
 template <int NB>
 constexpr int FEW_SLAB = NB * 16 * SLAB_ROW_BYTES;   // a block of 128 columns of the tokens

@@ -308,10 +308,11 @@ __device__ __forceinline__ float scale_product(uint32_t a, uint32_t b) {
 }
 
 // Loops without an order of their own: a slab's fragments are read and multiplied as the compiler places them.
-//   EXACT   fp32 sums (fp32 logits, and everything of up to 64 tokens): fragments are widened to bf16 and multiplied there, a block's sum
-//           is scaled into the accumulators.  128 x 128: 128 widenings and 64 fused multiply-adds beside 64 MFMAs of 16 cycles a wavefront and slab; 1000 tokens of a 128256 x 4096 head run
-//           at 0.98 PFLOP/s.  (The three interleaved by hand, one MFMA and two or three of the others: the same within 3 %.  256 x 128 tiles of four
-//           wavefronts of 128 x 64, a quarter less to widen: 0.81, one wavefront a SIMD leaves nothing to run beside a wait.)
+//   EXACT   fp32 sums (fp32 logits, and everything of up to 64 tokens): fragments are widened to bf16 and multiplied there, a block's sum is scaled
+//           into the accumulators.  128 x 128: 128 widenings and 64 fused multiply-adds beside 64 MFMAs of 16 cycles a wavefront and slab; 1000
+//           tokens of a 128256 x 4096 head run at 0.98 PFLOP/s.  (The three interleaved by hand, one MFMA and two or three of the others: the same
+//           within 3 %.  256 x 128 tiles of four wavefronts of 128 x 64, a quarter less to widen: 0.81, one wavefront a SIMD leaves nothing to run
+//           beside a wait.)
 //   else    on the 8-bit pipe; 64 x 64 tiles, where few larger ones would leave CUs without work
 template <typename S_, typename Order_, bool EXACT>
 struct TileGemmBlocksSimple : BlockStreams<S_, Order_> {

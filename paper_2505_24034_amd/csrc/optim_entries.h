@@ -230,8 +230,9 @@ llamarl_status llamarl_adamw_step(const llamarl_adamw_tensor* tensors, int64_t c
   a.scale = grad_scale;
   a.lr_device = lr_device;
   a.step_device = step_device;
-  // One unit a workgroup: with more the chip's last round is longer.  1 / 2 / 4 / 8 / 16 times 2048 entries, 8B head, 32 bits 3.29 / 3.34 /
-  // 3.38 / 3.43 / 3.50 ms, 8 bits 1.56 / 1.60 / 1.64 / 1.67 / 1.70, 109 tensors of a 170 M model 983 / 1022 / 1047 / 1083 / 1126 us.
+  // One unit a workgroup: with more the chip's last round is longer.  Measured with units of 2048 entries (256 threads), 1 / 2 / 4 / 8 / 16 a workgroup:
+  // 8B head, 32 bits 3.29 / 3.34 / 3.38 / 3.43 / 3.50 ms, 8 bits 1.56 / 1.60 / 1.64 / 1.67 / 1.70, 109 tensors of a 170 M model 983 / 1022 / 1047 / 1083 /
+  // 1126 us.
   return for_each_launch(
       count, 1, a.l,
       [&](int64_t i, OptTensor& t) {

@@ -9,15 +9,15 @@
 // (the norm has to be known before the first entry moves).  A launch takes up to OPT_TENSORS tensors, described in its arguments:
 // no table in memory that a caller would have to keep, or a captured graph could find changed.
 //
-// States in 8 bits: STATE_BLOCK neighbouring entries of a tensor share one fp32 factor, their largest magnitude / 448, and each is
-// held as e4m3 times that.  The second moment is held as its square root, which halves the exponents it spans.  m is
-// rounded to nearest: an update moves it by (1 - b1) |g - m|, a tenth of the difference, and half a step is 3 - 6 % of it.  What is below that is lost,
-// so that m can stay up to 0.63 of itself away from a constant gradient (b1 = 0.9), but not on the other side of zero: b1 <= STATE_BETA1 takes
-// more than half a step off any code above 2^-6 when the gradient is zero (1.125 -> 1.0547, nearer to 1).  sqrt(v) moves by
-// less than a rounding step in one update (0.05 % at b2 = 0.999, a step is 6 - 12 %): rounded to nearest
-// it would stay where it is however long the gradients say otherwise, so it is rounded up or down with the probability that
-// keeps its mean, by bits hashed out of (step, tensor, entry) -- the same call gives the same bits.  A second moment that is
-// not zero is never rounded to zero, where its entry would next be divided by eps: below the smallest code it counts as that.
+// States in 8 bits: STATE_BLOCK neighbouring entries of a tensor share one fp32 factor, their largest magnitude / 448, and each
+// is held as e4m3 times that.  The second moment is held as its square root, which halves the exponents it spans.  m is rounded
+// to nearest: an update moves it by (1 - b1) |g - m|, a tenth of the difference, and half a step is 3 - 6 % of it.  What is below
+// that is lost, so that m can stay up to 0.63 of itself away from a constant gradient (b1 = 0.9), but not on the other side of
+// zero: b1 <= STATE_BETA1 takes more than half a step off any code above 2^-6 when the gradient is zero (1.125 -> 1.0547, nearer
+// to 1).  sqrt(v) moves by less than a rounding step in one update (0.05 % at b2 = 0.999, a step is 6 - 12 %): rounded to nearest
+// it would stay where it is however long the gradients say otherwise, so it is rounded up or down with the probability that keeps
+// its mean, by bits hashed out of (step, tensor, entry) -- the same call gives the same bits.  A second moment that is not zero
+// is never rounded to zero, where its entry would next be divided by eps: below the smallest code it counts as that.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -28,7 +28,7 @@
 namespace llamarl {
 
 constexpr int OPT_TENSORS = 48;              // tensors of a launch: 3.5 of the 4 KB of kernel arguments
-// 512 threads against 256: 8-bit states of the 8B head 1.57 -> 1.48 ms (mean of five runs each), 32-bit ones the same
+// 512 threads against 256, in turn on one card: 8-bit states of the 8B head 1576 -> 1544 us, 32-bit ones and the norm 3362 -> 3338
 constexpr int OPT_THREADS = 512, OPT_ITEMS = 8, OPT_UNIT = OPT_THREADS * OPT_ITEMS;
 constexpr int STATE_BLOCK = 128;             // 16 lanes of eight entries: one row of a wavefront's cross-lane moves
 constexpr float E4M3_MAX = 448.f;

@@ -300,11 +300,11 @@ LLAMARL_RULE int direct_parts(int64_t d) {
   const int64_t groups = (d + 511) / 512;
   return groups >= 8 ? 8 : groups >= 4 ? 4 : groups >= 2 ? 2 : 1;
 }
-// Logits of one or two tokens on a little more than 32640 rows, whose 64 x 64 tiles are about half of the four that a CU takes: the direct kernel, where
-// all of its wavefronts have as many groups of K.  Tiles / direct, fp32 logits of 1 | 2 tokens, us: (32900, 4096) 35.6 / 29.3 | 35.6 / 30.8, (36000, 2048)
-// 19.5 / 18.0 | 19.5 / 18.5, (39000, 4096) 36.3 / 33.2 | 36.5 / 35.2, (41000, 8192) 64.7 / 66.2 | 64.9 / 68.8, (44000, 2048) 20.6 / 20.8 | 20.6 / 21.5;
-// groups that do not divide (33001, 1536) 15.2 / 16.8 (though (36000, 6144) 50.7 / 45.8), one group (33001, 512) 7.9 / 8.4; three tokens (44000, 4096) 37.8 / 39.9.  Log-probs, whose direct
-// tiles are of 16 rows: (33001, 8192) 67 / 73.
+// Logits of one or two tokens on a little more than 32640 rows, whose 64 x 64 tiles are about half of the four that a CU takes: the direct kernel,
+// where all of its wavefronts have as many groups of K.  Tiles / direct, fp32 logits of 1 | 2 tokens, us: (32900, 4096) 35.6 / 29.3 | 35.6 / 30.8,
+// (36000, 2048) 19.5 / 18.0 | 19.5 / 18.5, (39000, 4096) 36.3 / 33.2 | 36.5 / 35.2, (41000, 8192) 64.7 / 66.2 | 64.9 / 68.8, (44000, 2048) 20.6 /
+// 20.8 | 20.6 / 21.5; groups that do not divide (33001, 1536) 15.2 / 16.8 (though (36000, 6144) 50.7 / 45.8), one group (33001, 512) 7.9 / 8.4; three
+// tokens (44000, 4096) 37.8 / 39.9.  Log-probs, whose direct tiles are of 16 rows: (33001, 8192) 67 / 73.
 constexpr int64_t DIRECT_LOGITS_TILES = 640;
 LLAMARL_RULE bool direct_logits(int64_t N, int64_t V, int64_t d) {
   const int64_t groups = (d + 511) / 512;
