@@ -11,7 +11,10 @@
  * and what stands on either side of it: llamarl_grad_norm and
  * llamarl_adamw_step apply a model's gradients; llamarl_quantise_blocks,
  * llamarl_logits_blocks and llamarl_token_logprobs_blocks are the head in 8
- * bits, as a generator uses it between two updates.
+ * bits, as a generator uses it between two updates; llamarl_quantise_rows,
+ * llamarl_logits_rows and llamarl_token_logprobs_rows the same in integers;
+ * llamarl_rms_norm the norm in front of either, and llamarl_verify_drafts what
+ * a generator that drafts tokens does with the logits.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -441,6 +444,103 @@ size_t llamarl_logprobs_blocks_workspace_bytes(int64_t N, int64_t V);
 llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_scale, const void* W, const uint8_t* W_scale,
                                              const int32_t* targets, const uint8_t* mask, int64_t N, int64_t d, int64_t V,
                                              float* logp, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A head in 8-bit integers: a scale for each token and for each vocabulary row.
+ *     x[r,c] ~ scale[r] * q[r,c]
+ * llamarl_quantise_rows: scale = (largest magnitude of the row) / 127 and q = x / scale, both in fp32 and correctly rounded, q then to
+ * the nearest integer (ties to even): -127 .. 127.  A row below 2^-100 is zeros, with scale 0; one with an entry that is not finite is
+ * zeros with scale NaN.
+ *   x      in  [rows,cols] of type dt, dense; cols % 16 == 0, cols < 2^17; q: out int8 [rows,cols]; scale: out float [rows].  x and q 16-byte
+ *              aligned; none may overlap another
+ */
+llamarl_status llamarl_quantise_rows(const void* x, int64_t rows, int64_t cols, llamarl_dtype dt, int8_t* q, float* scale, void* stream);
+
+/*
+ * Logits under such a head (or any product of two such matrices):
+ *     z[t,v] = (sum_k H[t,k] W[v,k]) * W_scale[v] * H_scale[t]
+ * The sum is exact; it is rounded to fp32, multiplied twice, and rounded once more for bf16.
+ *   H, H_scale  in  int8 [N,d], float [N];  d % 16 == 0, d < 2^17, N * d < 2^31
+ *   W, W_scale  in  int8 [V,d], float [V];  V < 2^21
+ *   z           out [N,V] of type z_dt; apart from the operands
+ */
+llamarl_status llamarl_logits_rows(const int8_t* H, const float* H_scale, const int8_t* W, const float* W_scale, int64_t N, int64_t d,
+                                   int64_t V, llamarl_dtype z_dt, void* z, void* stream);
+
+/*
+ * llamarl_token_logprobs under such a head.  targets, mask, logp and lse as there; the logits never reach memory.
+ *   ws  scratch, >= llamarl_logprobs_rows_workspace_bytes(N, V), which does not fall as N or V grows (0 for sizes that no d allows)
+ * logp, lse and ws lie apart from each other and from the operands.
+ */
+size_t llamarl_logprobs_rows_workspace_bytes(int64_t N, int64_t V);
+llamarl_status llamarl_token_logprobs_rows(const int8_t* H, const float* H_scale, const int8_t* W, const float* W_scale,
+                                           const int32_t* targets, const uint8_t* mask, int64_t N, int64_t d, int64_t V,
+                                           float* logp, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Root-mean-square norm of the residual stream, in front of the head:
+ *     sum = x + residual (rounded to dt)        rstd = 1 / sqrt(mean(sum^2) + eps)        h = sum * rstd * weight
+ * Without a residual (NULL, as sum then is) it is x that is normalised.  Squares are summed in 64 bits, the rest is fp32; the norm is that of
+ * the sum as it is stored.
+ *   x, residual  in  [N,d] of type dt;  d at most 16384, a multiple of 8 (bf16) or 4 (fp32), of 16 for an output in 8 bits
+ *   weight       in  [d] of type w_dt
+ *   eps          positive
+ *   out          h is of type dt (h_scale NULL), or in 8 bits: what llamarl_quantise_blocks (block_rows 1; h_scale as there) or
+ *                llamarl_quantise_rows (h_scale float [N]) makes of the fp32 h
+ *   sum, h       out [N,d];  rstd: out float [N] or NULL, for the backward
+ * No output overlaps another array (INVALID_ARG).  A row with an entry that is not finite gives entries that are not, in its own row only.
+ */
+typedef enum { LLAMARL_NORM_SAME = 0, LLAMARL_NORM_E4M3_BLOCKS = 1, LLAMARL_NORM_INT8_ROWS = 2 } llamarl_norm_out;
+llamarl_status llamarl_rms_norm(const void* x, const void* residual, const void* weight, int64_t N, int64_t d, llamarl_dtype dt,
+                                llamarl_dtype w_dt, float eps, llamarl_norm_out out, void* sum, void* h, void* h_scale, float* rstd,
+                                void* stream);
+
+/*
+ * Its backward.  With n = s * rstd and g = dh * weight:
+ *     dx = rstd * (g - n * mean(g * n)) + dsum            dweight = sum over rows of dh * n
+ * dx is the gradient of x and of the residual alike; dsum what comes back to the sum itself.
+ *   dh, dsum  in  [N,d] of type dt; dsum may be NULL (= 0)
+ *   s         in  [N,d]: what was normalised (sum, or x without a residual);  rstd: in float [N]
+ *   dx        out [N,d] of type dt
+ *   dweight   out [d] of type dw_dt, or NULL: ws is not needed then
+ *   ws        scratch, >= llamarl_rms_norm_bwd_workspace_bytes(N, d), which does not fall as N grows
+ * Outputs and ws overlap no other array (INVALID_ARG).
+ */
+size_t llamarl_rms_norm_bwd_workspace_bytes(int64_t N, int64_t d);
+llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* weight, const float* rstd, const void* dsum, int64_t N,
+                                    int64_t d, llamarl_dtype dt, llamarl_dtype w_dt, void* dx, void* dweight, llamarl_dtype dw_dt,
+                                    void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Drafted tokens against the policy that is generated from.  Sequence b has n = draft_lens[b] drafts x_0 .. x_{n-1} (a smaller model's,
+ * or copied from the prompt), logits at each draft's place and at the one behind the last, and numbers u_0 .. u_K in [0, 1).  With
+ * p_i = softmax(logits / T) and q_i = softmax(draft_logits / T), or q_i all on x_i without draft_logits:
+ *     draft i is accepted while u_i q_i(x_i) < p_i(x_i)
+ *     the first that is not is replaced by a token out of max(p_i - q_i, 0), normalised (out of p_i where that is empty)
+ *     behind n accepted drafts comes a token out of p_n
+ * so the tokens are distributed as the policy's own, whatever the drafts are.  The last token is the first v, in the order of the vocabulary,
+ * with  sum_{w <= v} r(w) > u_K sum_w r(w), r what it is drawn from.  T = 0: p_i is all on the largest logit (the first of equal ones), and so is q_i on x_i.
+ * Distributions, sums and comparisons are in 64 bits.
+ *   logits        in  [B,K+1,V] of type dt; rows behind a sequence's last place are not read
+ *   draft_logits  in  [B,K,V] of type dt, or NULL
+ *   drafts        in  int32 [B,K] (may be NULL for K = 0);  one outside the vocabulary is refused, q_i has nothing on it then
+ *   draft_lens    in  int32 [B] or NULL (= K); taken as 0 where it is less and as K where it is more
+ *   temperature   in  float [B] or NULL (= 1)
+ *   uniforms      in  float [B,K+1]; the last one of a sequence draws its token.  Numbers below 0 count as 0, one that is 1 or more accepts
+                    nothing of p_i <= q_i and draws the last token of r; NaN accepts nothing and draws the first
+ *   tokens        out int32 [B,K+1]: accepted drafts, the token behind them, -1 from there on
+ *   accepted      out int32 [B]
+ *   logp          out float [B,K+1]: log p_i of the tokens (the generator's mu; 0 at T = 0), 0 from there on
+ *   ws            scratch, >= llamarl_verify_drafts_workspace_bytes(B, K, V), which falls with none of them
+ * A logit of -inf is a token that is never drawn.  A row without a distribution (a NaN, an infinite or nothing but -inf logits; T negative or not
+ * finite) accepts no draft, and if it is the last one's, its token is -1 and its logp NaN.  K is at most 127, B < 2^20, V < 2^21.
+ * Outputs and ws overlap no other array (INVALID_ARG).
+ */
+size_t llamarl_verify_drafts_workspace_bytes(int64_t B, int64_t K, int64_t V);
+llamarl_status llamarl_verify_drafts(const void* logits, const void* draft_logits, const int32_t* drafts, const int32_t* draft_lens,
+                                     const float* temperature, const float* uniforms, int64_t B, int64_t K, int64_t V,
+                                     llamarl_dtype dt, int32_t* tokens, int32_t* accepted, float* logp, void* ws, size_t ws_bytes,
+                                     void* stream);
 
 #ifdef __cplusplus
 }

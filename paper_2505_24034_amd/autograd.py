@@ -45,3 +45,35 @@ def aipo_loss(H, W, targets, mu_logp, adv, mask, rho=2.0, norm_mode=L.NORM_TOKEN
     the library before it is cast to W's dtype for autograd."""
     return _AipoLoss.apply(H, W, targets, mu_logp, adv, mask, float(rho), int(norm_mode), int(clip_mode),
                            float(eps_lo), float(eps_hi), dW_dtype)
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        h, s, rstd = L.rms_norm(x, weight, eps, residual=residual)
+        ctx.save_for_backward(s, weight, rstd)
+        ctx.set_materialize_grads(False)
+        ctx.summed = residual is not None
+        return (h, s) if ctx.summed else h
+
+    @staticmethod
+    def backward(ctx, g_h, g_s=None):
+        s, weight, rstd = ctx.saved_tensors
+        if g_h is None:                      # the sum alone was used
+            return g_s, None, g_s if ctx.summed else None, None
+        dx, dw = L.rms_norm_bwd(g_h.contiguous(), s, weight, rstd, dsum=None if g_s is None else g_s.contiguous(),
+                                want_dweight=ctx.needs_input_grad[1])
+        return dx, dw, dx if ctx.summed else None, None
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None):
+    """The norm in front of the head (`llamarl_rms_norm`): x, residual [..., d] and weight [d] (bf16 or fp32, contiguous, on the GPU) ->
+    h, or (h, x + residual) with a residual.  Gradients go to all three (`llamarl_rms_norm_bwd`)."""
+    shape = x.shape
+    rows = x.reshape(-1, shape[-1])
+    if residual is None:
+        return _RmsNorm.apply(rows, weight, None, float(eps)).view(shape)
+    if residual.shape != shape:
+        raise L.LlamarlError(L.ERR_INVALID_ARG, "residual must have the shape of x")
+    h, s = _RmsNorm.apply(rows, weight, residual.reshape(-1, shape[-1]), float(eps))
+    return h.view(shape), s.view(shape)

@@ -30,7 +30,10 @@ EXPORTS = ("llamarl_workspace_bytes", "llamarl_last_error", "llamarl_version", "
            "llamarl_offpolicy_loss_bwd_slice", "llamarl_bwd_workspace_bytes", "llamarl_offpolicy_loss_bwd_chunked",
            "llamarl_offpolicy_loss_bwd_device_scale", "llamarl_grad_norm_workspace_bytes", "llamarl_grad_norm",
            "llamarl_adamw_step", "llamarl_quantise_blocks", "llamarl_logits_blocks",
-           "llamarl_logprobs_blocks_workspace_bytes", "llamarl_token_logprobs_blocks")
+           "llamarl_logprobs_blocks_workspace_bytes", "llamarl_token_logprobs_blocks", "llamarl_quantise_rows",
+           "llamarl_logits_rows", "llamarl_logprobs_rows_workspace_bytes", "llamarl_token_logprobs_rows", "llamarl_rms_norm",
+           "llamarl_rms_norm_bwd_workspace_bytes", "llamarl_rms_norm_bwd", "llamarl_verify_drafts_workspace_bytes",
+           "llamarl_verify_drafts")
 
 
 class LlamarlError(RuntimeError):
@@ -127,6 +130,24 @@ def load():
     lib.llamarl_logprobs_blocks_workspace_bytes.argtypes = [i64, i64]
     lib.llamarl_token_logprobs_blocks.restype = ci
     lib.llamarl_token_logprobs_blocks.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.llamarl_quantise_rows.restype = ci
+    lib.llamarl_quantise_rows.argtypes = [vp, i64, i64, ci, vp, vp, vp]
+    lib.llamarl_logits_rows.restype = ci
+    lib.llamarl_logits_rows.argtypes = [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp]
+    lib.llamarl_logprobs_rows_workspace_bytes.restype = sz
+    lib.llamarl_logprobs_rows_workspace_bytes.argtypes = [i64, i64]
+    lib.llamarl_token_logprobs_rows.restype = ci
+    lib.llamarl_token_logprobs_rows.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.llamarl_rms_norm.restype = ci
+    lib.llamarl_rms_norm.argtypes = [vp, vp, vp, i64, i64, ci, ci, cf, ci, vp, vp, vp, vp, vp]
+    lib.llamarl_rms_norm_bwd_workspace_bytes.restype = sz
+    lib.llamarl_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+    lib.llamarl_rms_norm_bwd.restype = ci
+    lib.llamarl_rms_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i64, ci, ci, vp, vp, ci, vp, sz, vp]
+    lib.llamarl_verify_drafts_workspace_bytes.restype = sz
+    lib.llamarl_verify_drafts_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.llamarl_verify_drafts.restype = ci
+    lib.llamarl_verify_drafts.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, ci, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -399,3 +420,60 @@ def logprobs_blocks_workspace_bytes(N, V):
 def token_logprobs_blocks(H, H_scale, W, W_scale, targets, mask=None, ws=None, stream=None):
     """llamarl_token_logprobs_blocks: (logp [N], lse [N]) float32 of the tokens under an 8-bit head."""
     return (_native or _load_native()).token_logprobs_blocks(H, H_scale, W, W_scale, targets, mask, ws, _handle(stream))
+
+
+def quantise_rows(x, stream=None):
+    """llamarl_quantise_rows: x [R, C] (float32 or bfloat16) -> (q int8 [R, C], scale float32 [R])."""
+    return (_native or _load_native()).quantise_rows(x, _handle(stream))
+
+
+def logits_rows(H, H_scale, W, W_scale, dtype=torch.float32, out=None, stream=None):
+    """llamarl_logits_rows: H [N, d] and W [V, d] with their scales, as quantise_rows returns them -> logits [N, V] in dtype (or into
+    `out`, in its own)."""
+    return (_native or _load_native()).logits_rows(H, H_scale, W, W_scale, _storage(dtype), out, _handle(stream))
+
+
+def logprobs_rows_workspace_bytes(N, V):
+    return int(load().llamarl_logprobs_rows_workspace_bytes(N, V))
+
+
+def token_logprobs_rows(H, H_scale, W, W_scale, targets, mask=None, ws=None, stream=None):
+    """llamarl_token_logprobs_rows: (logp [N], lse [N]) float32 of the tokens under a head in 8-bit integers."""
+    return (_native or _load_native()).token_logprobs_rows(H, H_scale, W, W_scale, targets, mask, ws, _handle(stream))
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, stream=None):
+    """llamarl_rms_norm: x, residual [N, d], weight [d] (float32 or bfloat16) -> (h [N, d], sum [N, d], rstd [N]); sum is x itself
+    without a residual.  sum and rstd are what rms_norm_bwd takes."""
+    return (_native or _load_native()).rms_norm(x, weight, eps, residual, 0, _handle(stream))
+
+
+def rms_norm_blocks(x, weight, eps=1e-6, residual=None, stream=None):
+    """llamarl_rms_norm with its output as quantise_blocks(h, 1) holds it: (q float8_e4m3fn [N, d], scale float8_e8m0fnu, sum [N, d])."""
+    return (_native or _load_native()).rms_norm(x, weight, eps, residual, 1, _handle(stream))
+
+
+def rms_norm_rows(x, weight, eps=1e-6, residual=None, stream=None):
+    """llamarl_rms_norm with its output as quantise_rows(h) holds it: (q int8 [N, d], scale float32 [N], sum [N, d])."""
+    return (_native or _load_native()).rms_norm(x, weight, eps, residual, 2, _handle(stream))
+
+
+def rms_norm_bwd_workspace_bytes(N, d):
+    return int(load().llamarl_rms_norm_bwd_workspace_bytes(N, d))
+
+
+def rms_norm_bwd(dh, s, weight, rstd, dsum=None, dweight_dtype=None, want_dweight=True, ws=None, stream=None):
+    """llamarl_rms_norm_bwd: (dx [N, d], dweight [d] in dweight_dtype or weight's, None where it is not wanted); s and rstd as
+    rms_norm returned them, dsum the gradient of the sum."""
+    return (_native or _load_native()).rms_norm_bwd(dh, s, weight, rstd, dsum, _storage(dweight_dtype), want_dweight, ws, _handle(stream))
+
+
+def verify_drafts_workspace_bytes(B, K, V):
+    return int(load().llamarl_verify_drafts_workspace_bytes(B, K, V))
+
+
+def verify_drafts(logits, drafts, uniforms, draft_logits=None, draft_lens=None, temperature=None, ws=None, stream=None):
+    """llamarl_verify_drafts: logits [B, K + 1, V] (or [B (K + 1), V], as a head's logits come), drafts int32 [B, K], uniforms float32
+    [B, K + 1], draft_logits [B, K, V] in logits' type, draft_lens int32 [B], temperature float32 [B] -> (tokens int32 [B, K + 1],
+    accepted int32 [B], logp float32 [B, K + 1])."""
+    return (_native or _load_native()).verify_drafts(logits, drafts, uniforms, draft_logits, draft_lens, temperature, ws, _handle(stream))

@@ -49,6 +49,12 @@ struct QuantiseArgs {
   uint32_t* words;
   int groups;              // of 512 columns
 };
+// the wavefront's four exponents, one of each 16 lanes, as a word
+__device__ __forceinline__ uint32_t scale_word(int e) {
+  const int b = e + 127;
+  return (uint32_t)__builtin_amdgcn_readlane(b, 0) | (uint32_t)__builtin_amdgcn_readlane(b, 16) << 8 |
+         (uint32_t)__builtin_amdgcn_readlane(b, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane(b, 48) << 24;
+}
 // eight entries as they lie in memory
 template <typename T>
 struct Raw8;
@@ -105,9 +111,7 @@ __global__ __launch_bounds__(QUANT_THREADS) void k_quantise_rows(QuantiseArgs a)
     raw[i].get(x);
     const int e = block_exponent(row_max(magnitude8(x)));
     if (at[i] >= 0) *reinterpret_cast<u32x2*>(a.q + at[i]) = quantise8(x, e);
-    const uint32_t b = (uint32_t)(e + 127);
-    const uint32_t word = (uint32_t)__builtin_amdgcn_readlane((int)b, 0) | (uint32_t)__builtin_amdgcn_readlane((int)b, 16) << 8 |
-                          (uint32_t)__builtin_amdgcn_readlane((int)b, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)b, 48) << 24;
+    const uint32_t word = scale_word(e);
     if (lane == 0) a.words[(u - row * a.groups) * a.rows + row] = word;
   }
 }

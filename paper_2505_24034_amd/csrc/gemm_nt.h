@@ -147,6 +147,22 @@ __device__ __forceinline__ int tile_row_of(int r, int nb) {
 }
 
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
+// int8: a lane's 16 bytes are 16 consecutive k of the 16x16x64 MFMA, which takes as many cycles as the bf16 one above.  The
+// accumulators hold the bits of int32 sums; zeros are zeros.
+struct I8 {
+  typedef int8_t store_t;
+  typedef i32x4_t frag_t;
+  static constexpr int EPC = 16;
+};
+__device__ __forceinline__ void mma(const i32x4_t& a, const i32x4_t& b, i32x4_t& c) {
+  c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(const i32x4_t& a, const i32x4_t& b, f32x4_t& c) {
+  i32x4_t n = __builtin_bit_cast(i32x4_t, c);
+  mma(a, b, n);
+  c = __builtin_bit_cast(f32x4_t, n);
+}
+
 // buffer_load_dwordx4 ... lds, written out by hand.  The compiler's wait-count pass cannot tell which LDS bytes
 // an LDS-direct load will fill: with the builtin, transposing reads (ds_read_b64_tr_b16 carries no memory operand) and
 // reads through a computed stage address wait for ALL loads in flight, which serialises the loop.  Issued from inline

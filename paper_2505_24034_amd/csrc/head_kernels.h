@@ -234,6 +234,11 @@ template <typename G>
 __device__ __forceinline__ void scale_rows(G& g, const LogitsTile& t, int row) {
   if constexpr (HasScales<G>::value) g.set_scale_rows((int64_t)t.tv * G::Shape::BM, row);
 }
+// ... and those of integers make logits of their sums behind the main loop.
+template <typename G, typename = void>
+struct HasRowScales : std::false_type {};
+template <typename G>
+struct HasRowScales<G, std::void_t<decltype(G::ROW_SCALES)>> : std::true_type {};
 
 // f(std::integral_constant<int, column blocks of this wavefront>()): a kernel's walk over its tiles.  The wavefronts of a
 // workgroup may take different branches; all of them meet the same barriers.
@@ -336,6 +341,7 @@ __device__ __forceinline__ void fwd_tiles(const FwdArgs& a, G& g, TileSchedule<P
     // (or spill reload) issued before the slab requests turns into a wait for the requests themselves, and the
     // epilogue would start only when the slabs have arrived.
     LLAMARL_FENCE();
+    if constexpr (HasRowScales<G>::value) g.finish(acc, lp);
 
     if (rowsV < BM) {   // last vocab tile only (block-uniform): rows past V must not enter the softmax
 #pragma unroll

@@ -18,6 +18,9 @@
 #include "loss_kernels.h"
 #include "optim_kernels.h"
 #include "block_kernels.h"
+#include "norm_kernels.h"
+#include "row_kernels.h"
+#include "verify_kernels.h"
 
 using namespace llamarl;
 
@@ -868,3 +871,6 @@ llamarl_status llamarl_kl_shaped_rewards(const float* rewards, const float* logp
 
 #include "optim_entries.h"
 #include "block_entries.h"
+#include "norm_entries.h"
+#include "row_entries.h"
+#include "verify_entries.h"

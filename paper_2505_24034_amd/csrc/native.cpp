@@ -51,7 +51,7 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   return THPVariable_Unpack(o);
 }
 const char* dtype_name(at::ScalarType t) {
-  return t == at::kFloat ? "torch.float32" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32" : "torch.uint8";
+  return t == at::kFloat ? "torch.float32" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32" : t == at::kChar ? "torch.int8" : "torch.uint8";
 }
 llamarl_dtype dtype_code(const at::Tensor& t) {
   if (t.scalar_type() == at::kBFloat16) return LLAMARL_BF16;
@@ -615,6 +615,203 @@ PyObject* token_logprobs_blocks(PyObject* const* a) {
   return tuple({logp, lse});
 }
 
+// ---- the head in 8-bit integers --------------------------------------------------------------------------------------------
+void on_device_of(const at::Tensor& t, const at::Tensor& like, const char* name, const char* like_name) {
+  if (t.defined() && t.device() != like.device()) invalid(std::string(name) + " must be on the device of " + like_name);
+}
+struct RowMatrix {     // int8 [rows, cols] and its scales
+  at::Tensor q, scale;
+  RowMatrix(PyObject* m, const char* name, PyObject* s, const char* scale_name) : q(needed(m, at::kChar, name)), scale(needed(s, at::kFloat, scale_name)) {
+    if (q.dim() != 2 || scale.dim() != 1 || scale.size(0) != q.size(0))
+      invalid(std::string(name) + " must be a matrix with one entry of " + scale_name + " for each of its rows");
+    on_device_of(scale, q, scale_name, name);
+  }
+};
+struct RowHead {
+  RowMatrix H, W;
+  int64_t N, d, V;
+  RowHead(PyObject* const* a) : H(a[0], "H", a[1], "H_scale"), W(a[2], "W", a[3], "W_scale") {
+    N = H.q.size(0);
+    d = H.q.size(1);
+    V = W.q.size(0);
+    if (W.q.size(1) != d || W.q.device() != H.q.device()) invalid("H and W must have rows of one length, on one device");
+  }
+};
+
+// x, stream
+PyObject* quantise_rows(PyObject* const* a) {
+  const at::Tensor& x = tensor(a[0], "x");
+  const llamarl_dtype dt = dtype_code(x);
+  need(x, x.scalar_type(), "x");
+  if (x.dim() != 2) invalid("x must be a matrix");
+  const int64_t R = x.size(0), C = x.size(1);
+  const c10::DeviceGuard on(x.device());
+  const CallStream st(a[1], x);
+  const at::Tensor q = empty(x, {R, C}, at::kChar), scale = empty(x, {R});
+  check(unlocked([&] { return llamarl_quantise_rows(ptr(x), R, C, dt, ptr<int8_t>(q), ptr<float>(scale), st.handle); }));
+  st.returns(q, scale);
+  return tuple({q, scale});
+}
+
+// H, H_scale, W, W_scale, dtype code, out, stream
+PyObject* logits_rows(PyObject* const* a) {
+  const RowHead x(a);
+  const c10::DeviceGuard on(x.H.q.device());
+  const CallStream st(a[6], x.H.q);
+  at::Tensor z;
+  if (a[5] != Py_None) {
+    z = tensor(a[5], "out");
+    need(z, z.scalar_type(), "out");
+    if (z.dim() != 2 || z.size(0) != x.N || z.size(1) != x.V || z.device() != x.H.q.device()) invalid("out must be [N, V] on the device of H");
+  } else {
+    z = empty(x.H.q, {x.N, x.V}, integer(a[4]) == LLAMARL_BF16 ? at::kBFloat16 : at::kFloat);
+  }
+  const llamarl_dtype dt = dtype_code(z);
+  check(unlocked([&] {
+    return llamarl_logits_rows(ptr<int8_t>(x.H.q), ptr<float>(x.H.scale), ptr<int8_t>(x.W.q), ptr<float>(x.W.scale), x.N, x.d, x.V, dt, ptr(z),
+                               st.handle);
+  }));
+  if (a[5] == Py_None) st.returns(z);
+  else bump(z);
+  return THPVariable_Wrap(z);
+}
+
+// H, H_scale, W, W_scale, targets, mask, ws, stream
+PyObject* token_logprobs_rows(PyObject* const* a) {
+  const RowHead x(a);
+  const at::Tensor targets = needed(a[4], at::kInt, "targets"), mask = optional(a[5], at::kByte, "mask");
+  if (targets.numel() != x.N || (mask.defined() && mask.numel() != x.N)) invalid("targets and mask must have N entries");
+  on_device_of(targets, x.H.q, "targets", "H");
+  on_device_of(mask, x.H.q, "mask", "H");
+  const c10::DeviceGuard on(x.H.q.device());
+  const CallStream st(a[7], x.H.q);
+  const at::Tensor logp = empty(targets, {x.N}), lse = empty(targets, {x.N});
+  const at::Tensor ws = workspace(a[6], llamarl_logprobs_rows_workspace_bytes(x.N, x.V), targets);
+  on_device_of(ws.is_cuda() ? ws : at::Tensor(), x.H.q, "ws", "H");
+  check(unlocked([&] {
+    return llamarl_token_logprobs_rows(ptr<int8_t>(x.H.q), ptr<float>(x.H.scale), ptr<int8_t>(x.W.q), ptr<float>(x.W.scale), ptr<int32_t>(targets),
+                                       ptr<uint8_t>(mask), x.N, x.d, x.V, ptr<float>(logp), ptr<float>(lse), ptr(ws), (size_t)ws.nbytes(),
+                                       st.handle);
+  }));
+  st.returns(logp, lse);
+  return tuple({logp, lse});
+}
+
+// ---- the norm in front of it --------------------------------------------------------------------------------------------------
+struct NormRows {      // [N, d] and weight [d]
+  at::Tensor x, w;
+  llamarl_dtype dt, w_dt;
+  int64_t N, d;
+  NormRows(PyObject* o, const char* name, PyObject* weight) : x(tensor(o, name)), w(tensor(weight, "weight")) {
+    dt = dtype_code(x);
+    w_dt = dtype_code(w);
+    need(x, x.scalar_type(), name);
+    need(w, w.scalar_type(), "weight");
+    if (x.dim() != 2 || w.dim() != 1 || w.size(0) != x.size(1)) invalid(std::string(name) + " must be [N, d] and weight [d]");
+    on_device_of(w, x, "weight", name);
+    N = x.size(0);
+    d = x.size(1);
+  }
+  at::Tensor beside(PyObject* o, const char* name) const {      // of x's type and shape, or None
+    const at::Tensor t = optional(o, x.scalar_type(), name);
+    if (t.defined() && t.sizes() != x.sizes()) invalid(std::string(name) + " must have the shape of the rows");
+    on_device_of(t, x, name, "the rows");
+    return t;
+  }
+};
+
+// x, weight, eps, residual, output (llamarl_norm_out), stream
+PyObject* rms_norm(PyObject* const* a) {
+  const NormRows r(a[0], "x", a[1]);
+  const float eps = (float)real(a[2]);
+  const at::Tensor residual = r.beside(a[3], "residual");
+  const llamarl_norm_out out = (llamarl_norm_out)integer(a[4]);
+  const c10::DeviceGuard on(r.x.device());
+  const CallStream st(a[5], r.x);
+  at::Tensor sum, scale, rstd;
+  if (residual.defined()) sum = empty(r.x, {r.N, r.d}, r.x.scalar_type());
+  const at::Tensor h = empty(r.x, {r.N, r.d}, out == LLAMARL_NORM_SAME ? r.x.scalar_type() : out == LLAMARL_NORM_E4M3_BLOCKS ? at::kFloat8_e4m3fn : at::kChar);
+  if (out == LLAMARL_NORM_SAME) rstd = empty(r.x, {r.N});
+  else if (out == LLAMARL_NORM_E4M3_BLOCKS) scale = empty(r.x, {scale_groups(r.d), r.N, 4}, at::kFloat8_e8m0fnu);
+  else scale = empty(r.x, {r.N});
+  check(unlocked([&] {
+    return llamarl_rms_norm(ptr(r.x), ptr(residual), ptr(r.w), r.N, r.d, r.dt, r.w_dt, eps, out, ptr(sum), ptr(h), ptr(scale), ptr<float>(rstd),
+                            st.handle);
+  }));
+  st.returns(h, rstd.defined() ? rstd : scale);
+  if (sum.defined()) st.returns(sum);
+  else sum = r.x;
+  return rstd.defined() ? tuple({h, sum, rstd}) : tuple({h, scale, sum});
+}
+
+// dh, s, weight, rstd, dsum, dweight dtype code, dweight wanted, ws, stream
+PyObject* rms_norm_bwd(PyObject* const* a) {
+  const NormRows r(a[1], "s", a[2]);
+  const at::Tensor dh = r.beside(a[0], "dh"), rstd = needed(a[3], at::kFloat, "rstd"), dsum = r.beside(a[4], "dsum");
+  if (!dh.defined()) invalid("dh must be given");
+  if (rstd.numel() != r.N) invalid("rstd must have N entries");
+  on_device_of(rstd, r.x, "rstd", "the rows");
+  const int64_t code = integer(a[5]);
+  const int wanted = PyObject_IsTrue(a[6]);
+  if (wanted < 0) throw Raised{};
+  const c10::DeviceGuard on(r.x.device());
+  const CallStream st(a[8], r.x);
+  const at::Tensor dx = empty(r.x, {r.N, r.d}, r.x.scalar_type());
+  at::Tensor dw, ws;
+  if (wanted) {
+    dw = empty(r.x, {r.d}, code < 0 ? r.w.scalar_type() : code == LLAMARL_BF16 ? at::kBFloat16 : at::kFloat);
+    ws = workspace(a[7], llamarl_rms_norm_bwd_workspace_bytes(r.N, r.d), r.x);
+    on_device_of(ws.is_cuda() ? ws : at::Tensor(), r.x, "ws", "the rows");
+  }
+  check(unlocked([&] {
+    return llamarl_rms_norm_bwd(ptr(dh), ptr(r.x), ptr(r.w), ptr<float>(rstd), ptr(dsum), r.N, r.d, r.dt, r.w_dt, ptr(dx), ptr(dw),
+                                wanted ? dtype_code(dw) : LLAMARL_F32, ptr(ws), wanted ? (size_t)ws.nbytes() : 0, st.handle);
+  }));
+  st.returns(dx);
+  if (wanted) {
+    st.returns(dw);
+    return tuple({dx, dw});
+  }
+  PyObject* x = THPVariable_Wrap(dx);
+  if (x == nullptr) throw Raised{};
+  return Py_BuildValue("NO", x, Py_None);
+}
+
+// ---- drafted tokens ------------------------------------------------------------------------------------------------------------
+// logits, drafts, uniforms, draft_logits, draft_lens, temperature, ws, stream
+PyObject* verify_drafts(PyObject* const* a) {
+  const at::Tensor& z = tensor(a[0], "logits");
+  const llamarl_dtype dt = dtype_code(z);
+  need(z, z.scalar_type(), "logits");
+  const at::Tensor &drafts = needed(a[1], at::kInt, "drafts"), &u = needed(a[2], at::kFloat, "uniforms");
+  if (drafts.dim() != 2) invalid("drafts must be [B, K]");
+  const int64_t B = drafts.size(0), K = drafts.size(1);
+  if (u.dim() != 2 || u.size(0) != B || u.size(1) != K + 1) invalid("uniforms must be [B, K + 1]");
+  if (z.dim() == 3 ? z.size(0) != B || z.size(1) != K + 1 : z.dim() != 2 || z.size(0) != B * (K + 1)) invalid("logits must be [B, K + 1, V] or [B (K + 1), V]");
+  const int64_t V = z.size(z.dim() - 1);
+  const at::Tensor y = optional(a[3], z.scalar_type(), "draft_logits"), lens = optional(a[4], at::kInt, "draft_lens"),
+                   temperature = optional(a[5], at::kFloat, "temperature");
+  if (y.defined() && (y.dim() == 3 ? y.size(0) != B || y.size(1) != K : y.dim() != 2 || y.size(0) != B * K)) invalid("draft_logits must be [B, K, V] or [B K, V]");
+  if (y.defined() && y.size(y.dim() - 1) != V) invalid("draft_logits must have the vocabulary of logits");
+  if ((lens.defined() && lens.numel() != B) || (temperature.defined() && temperature.numel() != B)) invalid("draft_lens and temperature must have B entries");
+  on_device_of(drafts, z, "drafts", "logits");
+  on_device_of(u, z, "uniforms", "logits");
+  on_device_of(y, z, "draft_logits", "logits");
+  on_device_of(lens, z, "draft_lens", "logits");
+  on_device_of(temperature, z, "temperature", "logits");
+  const c10::DeviceGuard on(z.device());
+  const CallStream st(a[7], z);
+  const at::Tensor tokens = empty(z, {B, K + 1}, at::kInt), accepted = empty(z, {B}, at::kInt), logp = empty(z, {B, K + 1});
+  const at::Tensor ws = workspace(a[6], llamarl_verify_drafts_workspace_bytes(B, K, V), z);
+  on_device_of(ws.is_cuda() ? ws : at::Tensor(), z, "ws", "logits");
+  check(unlocked([&] {
+    return llamarl_verify_drafts(ptr(z), K > 0 ? ptr(y) : nullptr, ptr<int32_t>(drafts), ptr<int32_t>(lens), ptr<float>(temperature), ptr<float>(u), B, K,
+                                 V, dt, ptr<int32_t>(tokens), ptr<int32_t>(accepted), ptr<float>(logp), ptr(ws), (size_t)ws.nbytes(), st.handle);
+  }));
+  st.returns(tokens, accepted, logp);
+  return tuple({tokens, accepted, logp});
+}
+
 // The rules by which the library cuts and deals out its work (tile_rules.h), for tests.
 // tiles_m, tiles_n, workgroups: the tiles (row * tiles_n + column) each workgroup of a logits kernel takes, in order
 PyObject* tile_walk(PyObject* const* a) {
@@ -676,6 +873,13 @@ PyObject* block_logits_plan(PyObject* const* a) {
   return Py_BuildValue("iLi", (int)p.tile, (long long)p.rows, (int)p.rest);
 }
 
+// N, V, d: kernel (RowTile) of a product with a head in 8-bit integers, rows of its tiles of partials, floats of their planes
+PyObject* row_plan(PyObject* const* a) {
+  const int64_t N = integer(a[0]), V = integer(a[1]);
+  const llamarl::RowTile t = llamarl::row_tile(N, V);
+  return Py_BuildValue("iiL", (int)t, llamarl::row_tile_rows(t, integer(a[2])), (long long)llamarl::row_partials(N, V));
+}
+
 template <PyObject* (*F)(PyObject* const*), int NARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -703,7 +907,8 @@ PyMethodDef g_methods[] = {
     ENTRY(token_logprobs, 6), ENTRY(token_logprobs_partial, 8), ENTRY(merge_partials, 4), ENTRY(offpolicy_loss_fwd, 15),
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
     ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
-    ENTRY(token_logprobs_blocks, 8), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(token_logprobs_blocks, 8), ENTRY(quantise_rows, 2), ENTRY(logits_rows, 7), ENTRY(token_logprobs_rows, 8), ENTRY(rms_norm, 6),
+    ENTRY(rms_norm_bwd, 9), ENTRY(verify_drafts, 8), ENTRY(row_plan, 3), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

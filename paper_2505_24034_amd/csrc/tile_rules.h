@@ -356,4 +356,26 @@ LLAMARL_RULE int64_t block_partials(int64_t N, int64_t V) {
   return large > few ? (large > s ? large : s) : few > s ? few : s;
 }
 
+// ---- heads in 8-bit integers (row_kernels.h) --------------------------------------------------------------------------------
+// Which kernel a product of N tokens with V rows of W takes.
+enum RowTile { ROW_DIRECT, ROW_64, ROW_128, ROW_256 };
+constexpr int64_t ROW_64_TILES = 256;
+LLAMARL_RULE RowTile row_tile(int64_t N, int64_t V) {
+  if (N <= DIRECT_TOKENS) return ROW_DIRECT;
+  if (tile_count(N, V, 128) < ROW_64_TILES) return ROW_64;
+  return N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? ROW_256 : ROW_128;
+}
+// rows of W that a tile of partials has
+LLAMARL_RULE int row_tile_rows(RowTile t, int64_t d) {
+  const int direct = DIRECT_WAVES / direct_parts(d) * 16;
+  return t == ROW_256 ? 256 : t == ROW_128 ? 128 : t == ROW_64 ? 64 : direct < 64 ? direct : 64;
+}
+// Floats of a plane of partials that serves any call of up to N tokens and V rows, see block_partials.
+LLAMARL_RULE int64_t row_partials(int64_t N, int64_t V) {
+  const int64_t n_pad = (N + 63) / 64 * 64;
+  const int64_t large = (V + 127) / 128 * n_pad, small = (V + 63) / 64 * n_pad, few = (V + 15) / 16 * 64;
+  const int64_t most = 256 * ROW_64_TILES, s = small < most ? small : most;
+  return large > few ? (large > s ? large : s) : few > s ? few : s;
+}
+
 }  // namespace llamarl
