@@ -5,30 +5,31 @@ namespace {
 
 struct VerifyWs {
   int64_t rows, chunks;
-  size_t off_s, off_i, off_r, off_p, total;
+  size_t off_at, off_sums, off_ticket, total;
 };
 VerifyWs verify_ws(int64_t B, int64_t K, int64_t V) {
   VerifyWs w;
   w.rows = B * (2 * K + 1);
   w.chunks = (V + VERIFY_CHUNK - 1) / VERIFY_CHUNK;
-  w.off_s = (size_t)round_up(w.rows * w.chunks * 4, 256);
-  w.off_i = w.off_s + (size_t)round_up(w.rows * w.chunks * 8, 256);
-  w.off_r = w.off_i + (size_t)round_up(B * (K + 1) * w.chunks * 4, 256);
-  w.off_p = w.off_r + (size_t)round_up(B * w.chunks * 8, 256);
-  w.total = w.off_p + (size_t)round_up(B * w.chunks * 8, 256);
+  w.off_at = (size_t)round_up(w.rows * w.chunks * (int64_t)sizeof(VerifyPart), 256);
+  w.off_sums = w.off_at + (size_t)round_up(w.rows * 4, 256);
+  w.off_ticket = w.off_sums + (size_t)round_up(B * w.chunks * (VERIFY_CHUNK / VERIFY_PART) * 8, 256);
+  w.total = w.off_ticket + (size_t)round_up(B * 4, 256);
   return w;
 }
 bool verify_fits(int64_t B, int64_t K, int64_t V) {
   return B > 0 && K >= 0 && V > 0 && K <= VERIFY_MOST_DRAFTS && V < BLOCK_MOST_ROWS && B < (int64_t)1 << 20 &&
          B * (2 * K + 1) * ((V + VERIFY_CHUNK - 1) / VERIFY_CHUNK) < ((int64_t)1 << 32) / VERIFY_THREADS;
 }
+constexpr int VERIFY_MOST_AT_ONCE = 8, VERIFY_MOST_EACH = 4;
 template <typename T>
 llamarl_status launch_verify(const VerifyArgs& a, int64_t rows, hipStream_t st) {
-  k_verify_rows<T><<<dim3((unsigned)(rows * a.chunks)), dim3(VERIFY_THREADS), 0, st>>>(a);
+  // Chunks of a workgroup: one where that fills the chip no more than a few times over, and then its logits are asked for before it knows whether
+  // somebody wants them.
+  const int64_t each = std::min<int64_t>(std::max<int64_t>(rows * a.chunks / persistent_grid((int64_t)1 << 30, VERIFY_MOST_AT_ONCE), 1), VERIFY_MOST_EACH);
+  k_verify_rows<T><<<dim3((unsigned)(rows * ((a.chunks + each - 1) / each))), dim3(VERIFY_THREADS), 0, st>>>(a, (int)each, each == 1);
   HIP_TRY(hipGetLastError());
-  k_verify_sums<T><<<dim3((unsigned)(a.B * a.chunks)), dim3(VERIFY_THREADS), 0, st>>>(a);
-  HIP_TRY(hipGetLastError());
-  k_verify_pick<T><<<dim3((unsigned)a.B), dim3(PICK_THREADS), 0, st>>>(a);
+  k_verify_pick<T><<<dim3((unsigned)(a.B * a.chunks)), dim3(VERIFY_THREADS), 0, st>>>(a);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
@@ -62,8 +63,8 @@ llamarl_status llamarl_verify_drafts(const void* logits, const void* draft_logit
     return fail(LLAMARL_ERR_INVALID_ARG, "outputs and workspace must not overlap another array");
   char* base = static_cast<char*>(ws);
   const VerifyArgs a = {logits, draft_logits, drafts, draft_lens, temperature, uniforms, V, (int)B, (int)K, (int)w.chunks,
-                        reinterpret_cast<float*>(base), reinterpret_cast<double*>(base + w.off_s), reinterpret_cast<int32_t*>(base + w.off_i),
-                        reinterpret_cast<double*>(base + w.off_r), reinterpret_cast<double*>(base + w.off_p), tokens, accepted, logp};
+                        reinterpret_cast<VerifyPart*>(base), reinterpret_cast<float*>(base + w.off_at), reinterpret_cast<double*>(base + w.off_sums),
+                        reinterpret_cast<unsigned int*>(base + w.off_ticket), tokens, accepted, logp};
   const int64_t rows = draft_logits ? w.rows : slots;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return dt == LLAMARL_BF16 ? launch_verify<uint16_t>(a, rows, st) : launch_verify<float>(a, rows, st);

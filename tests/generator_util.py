@@ -80,7 +80,7 @@ def verify(logits, drafts, u, draft_logits=None, lens=None, temps=None):
                         tokens[b, i], logp[b, i] = x, (0.0 if T == 0 else math.log(p[x]))
                         continue
                     r = np.maximum(p - q, 0.0)
-                    r = r if r.sum() > 0 else p
+                    r = r if r.sum() > 2.0 ** -40 else p                   # less is the rounding of p and q
                 else:
                     r = None
             accepted[b] = i
