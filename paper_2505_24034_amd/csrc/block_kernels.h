@@ -185,7 +185,8 @@ struct BlockLogitsArgs {
 // (2000, 65066, 528) 185 us instead of 173, (1714, 5653, 448) 28.4 instead of 24.8, and 64 of fp32: (2000, 65066, 528) 310
 // instead of 295.
 typedef int i32x4_any __attribute__((ext_vector_type(4), aligned(2)));      // rows of z start wherever V puts them
-template <typename S, typename Out>
+// PACK: bf16 by the conversion instruction (the same bits; a NaN's may differ).
+template <typename S, typename Out, bool PACK = false>
 struct TileStore {
   static constexpr bool BF16_OUT = sizeof(Out) == 2;
   // logits of a lane's store, and of 128 bytes (64 x 64 tiles: 64, all that four of them leave of a CU's LDS)
@@ -212,7 +213,9 @@ struct TileStore {
         for (int i = 0; i < BLOCKS; ++i) {
           const f32x4_t x = acc[part * BLOCKS + i][j];
           char* at = own + l16 * PITCH + (16 * i + 4 * g) * (int)sizeof(Out);
-          if constexpr (BF16_OUT) {
+          if constexpr (BF16_OUT && PACK) {
+            *reinterpret_cast<u32x2*>(at) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+          } else if constexpr (BF16_OUT) {
             uint16_t b[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) b[r] = float_to_bf16_bits(x[r]);

@@ -111,6 +111,11 @@ __device__ __forceinline__ void clear(f32x4_t (&acc)[M][N]) {
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[i][j] = f32x4_t{z, z, z, z};
 }
+// Loops of integers (row_kernels.h) have a scale for each row of either operand and make logits of their sums behind the main loop.
+template <typename G, typename = void>
+struct HasRowScales : std::false_type {};
+template <typename G>
+struct HasRowScales<G, std::void_t<decltype(G::ROW_SCALES)>> : std::true_type {};
 // One tile's main loop; a wavefront with no part in the tile only takes part in its loads (256-row loops).  nb: its column
 // blocks; counted: the loop's COUNTED_STORES were issued since the tile was fetched (TileGemm::run).
 template <typename G, int nb>
@@ -127,6 +132,7 @@ __device__ __forceinline__ void run_tile(G& g, char* smem, f32x4_t (&acc)[G::Sha
   if constexpr (nb == 0) {
   } else if constexpr (std::is_same<G, Logits256>::value || std::is_same<G, Logits256Turned>::value ||
                        std::is_same<G, Logits256Ring>::value || std::is_same<G, LogitsWide>::value) g.run(smem, acc, counted);
+  else if constexpr (HasRowScales<G>::value) g.run(smem, acc, counted);
   else if constexpr (G::HALVES && !G::KMAJOR) g.template run<nb>(smem, acc, counted);
   else if constexpr (G::HALVES) g.template run<nb>(smem, acc);
   else g.run(smem, acc);
@@ -234,11 +240,6 @@ template <typename G>
 __device__ __forceinline__ void scale_rows(G& g, const LogitsTile& t, int row) {
   if constexpr (HasScales<G>::value) g.set_scale_rows((int64_t)t.tv * G::Shape::BM, row);
 }
-// ... and those of integers make logits of their sums behind the main loop.
-template <typename G, typename = void>
-struct HasRowScales : std::false_type {};
-template <typename G>
-struct HasRowScales<G, std::void_t<decltype(G::ROW_SCALES)>> : std::true_type {};
 
 // f(std::integral_constant<int, column blocks of this wavefront>()): a kernel's walk over its tiles.  The wavefronts of a
 // workgroup may take different branches; all of them meet the same barriers.

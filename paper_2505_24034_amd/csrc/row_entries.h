@@ -47,7 +47,7 @@ llamarl_status launch_row_direct(RowFewArgs a, hipStream_t st) {
 }
 template <typename G, typename Out>
 llamarl_status launch_row_logits(RowLogitsArgs a, hipStream_t st) {
-  a.tiles_v = (int)((a.V + G::Shape::BM - 1) / G::Shape::BM);
+  a.tiles_v = (int)((a.v_end - a.v_first + G::Shape::BM - 1) / G::Shape::BM);
   a.tiles_t = (int)((a.N + G::Shape::BN - 1) / G::Shape::BN);
   constexpr int LDS = G::LDS_BYTES + TileStore<typename G::Shape, Out>::LDS_BYTES;
   static_assert(LDS * G::GROUPS_PER_CU <= 160 * 1024, "LDS of a CU");
@@ -58,7 +58,8 @@ llamarl_status launch_row_logits(RowLogitsArgs a, hipStream_t st) {
 }
 template <typename Out>
 llamarl_status launch_row_tiles(const RowLogitsArgs& a, RowTile t, hipStream_t st) {
-  return (t == ROW_256 ? launch_row_logits<Rows256, Out> : t == ROW_128 ? launch_row_logits<Rows128, Out> : launch_row_logits<Rows64, Out>)(a, st);
+  return (t == ROW_256 ? launch_row_logits<Rows256Stored, Out> : t == ROW_128 ? launch_row_logits<Rows128, Out>
+          : t == ROW_64 ? launch_row_logits<Rows64, Out> : launch_row_logits<Rows64Deep, Out>)(a, st);
 }
 template <typename G>
 llamarl_status launch_row_partials(const FwdArgs& a, const RowHead& x, hipStream_t st) {
@@ -117,15 +118,20 @@ llamarl_status llamarl_logits_rows(const int8_t* H, const float* H_scale, const 
   if (any_overlap({{z, N * V * (int64_t)esize(z_dt)}}, {{H, N * d}, {H_scale, N * 4}, {W, V * d}, {W_scale, V * 4}}))
     return fail(LLAMARL_ERR_INVALID_ARG, "z must not overlap an operand");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const RowTile tile = row_tile(N, V);
-  if (tile == ROW_DIRECT) {
+  const RowLogits plan = row_logits(N, V, d);
+  if (plan.tile == ROW_DIRECT) {
     RowFewArgs f = {};
     f.x = x;
     f.few.N = N; f.few.d = d; f.few.V = V; f.few.z = z;
     return z_dt == LLAMARL_F32 ? launch_row_direct<float>(f, st) : launch_row_direct<uint16_t>(f, st);
   }
-  const RowLogitsArgs a = {x, N, d, V, 0, 0, z};
-  return z_dt == LLAMARL_F32 ? launch_row_tiles<float>(a, tile, st) : launch_row_tiles<uint16_t>(a, tile, st);
+  RowLogitsArgs a = {x, N, d, V, 0, plan.rows, 0, 0, z};
+  const auto launch = [&](RowTile t) { return z_dt == LLAMARL_F32 ? launch_row_tiles<float>(a, t, st) : launch_row_tiles<uint16_t>(a, t, st); };
+  const llamarl_status first = launch(plan.tile);
+  if (first != LLAMARL_OK || plan.rows == V) return first;
+  a.v_first = plan.rows;
+  a.v_end = V;
+  return launch(plan.rest);
 }
 
 size_t llamarl_logprobs_rows_workspace_bytes(int64_t N, int64_t V) {
@@ -170,7 +176,8 @@ llamarl_status llamarl_token_logprobs_rows(const int8_t* H, const float* H_scale
     f.few.N = N; f.few.d = d; f.few.V = V; f.few.f = a;
     s = launch_row_direct<void>(f, st);
   } else {
-    s = (tile == ROW_256 ? launch_row_partials<Rows256> : tile == ROW_128 ? launch_row_partials<Rows128> : launch_row_partials<Rows64>)(a, x, st);
+    s = (tile == ROW_256 ? launch_row_partials<Rows256> : tile == ROW_128 ? launch_row_partials<Rows128>
+         : tile == ROW_64 ? launch_row_partials<Rows64> : launch_row_partials<Rows64Deep>)(a, x, st);
   }
   if (s != LLAMARL_OK) return s;
   return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);

@@ -131,6 +131,57 @@ struct RowHead {
   const float* h_scale;
   const float* w_scale;
 };
+// TileGemmSmall with its slabs taken round a ring (SlabRing), for W that streams from memory: workgroups start at slabs of their own.
+template <typename S_, int NSTAGE, int GROUPS_PER_CU_>
+struct TileGemmRing : TileGemmSmall<I8, S_, NSTAGE, GROUPS_PER_CU_> {
+  typedef TileGemmSmall<I8, S_, NSTAGE, GROUPS_PER_CU_> Base;
+  typedef S_ S;
+  using Base::BK;
+  using Base::K;
+  using Base::la;
+  using Base::lb;
+  SlabRing order;
+  __device__ __forceinline__ void issue(char* stage, int kt) const {
+    const int lane = threadIdx.x & 63, wave = wave_id(), k0 = kt * BK >= K ? kt * BK : order.template k<BK>(kt, K);      // past K: zeros, no traffic
+    la.issue(stage, k0, K, wave, lane);
+    lb.issue(stage + S::SLAB_A_BYTES, k0, K, wave, lane);
+  }
+  __device__ __forceinline__ void issue_first(char* smem, int) const {
+#pragma unroll
+    for (int i = 0; i < NSTAGE - 1; ++i) issue(smem + i * S::STAGE_BYTES, i);
+  }
+  template <bool NEAR>
+  __device__ __forceinline__ void setup_gathered(const void* A_tile, int64_t lda, int rowsA, const void* B_base, int64_t ldb, int rowsB,
+                                                 int64_t K_, const int (&grow)[Base::LoaderB::ITERS], int64_t b_total, int turn) {
+    Base::template setup_gathered<NEAR>(A_tile, lda, rowsA, B_base, ldb, rowsB, K_, grow, b_total, turn);
+    order.template init<BK>(K, turn);
+  }
+  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[S::MB][S::NB]) {
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int g = lane >> 4, l16 = lane & 15, sw = swizzle(l16);
+    int a_addr[2], b_addr[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      a_addr[ks] = (S::wave_row(wave) * S::WAVE_M + l16) * SLAB_ROW_BYTES + (((4 * ks + g) ^ sw) * 16);
+      b_addr[ks] = S::SLAB_A_BYTES + (S::wave_col(wave) * S::WAVE_N + l16) * SLAB_ROW_BYTES + (((4 * ks + g) ^ sw) * 16);
+    }
+    Base::clear(acc);
+    const int nk = (K + BK - 1) / BK;
+    wait_vmcnt0();
+    __syncthreads();
+    int st = 0;
+    for (int kt = 0; kt < nk; ++kt) {                // see TileGemmSmall::run
+      if (kt > 0) {
+        wait_vmcnt<Base::LOADS * (NSTAGE - 2)>();
+        __syncthreads();
+      }
+      issue(smem + (st == 0 ? NSTAGE - 1 : st - 1) * S::STAGE_BYTES, kt + NSTAGE - 1);
+      Base::slab(smem + st * S::STAGE_BYTES, a_addr, b_addr, acc);
+      st = st == NSTAGE - 1 ? 0 : st + 1;
+    }
+  }
+};
+
 // A loop of bf16's on bytes, and the scales of its tiles: a tile's rows' and columns' come to LDS with its first slabs, 64 words a
 // wavefront, two tiles' in turn (an epilogue reads them while the next tile's are under way).
 template <typename Loop>
@@ -166,9 +217,10 @@ struct RowScaled : Loop {
     const uint32_t at = rows ? (uint32_t)min(v0 + wave * 64 + lane, V - 1) : (uint32_t)row;
     lds_dma4(lds_address(scales) + (uint32_t)(turn * SCALES_BYTES + wave * 256), at * 4u, rs);
   }
-  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[Shape::MB][Shape::NB]) {
+  __device__ __forceinline__ void run(char* smem, f32x4_t (&acc)[Shape::MB][Shape::NB], bool counted) {
     of_tile = turn;
-    Loop::run(smem, acc);
+    if constexpr (Loop::HAS_IDLE) Loop::run(smem, acc, counted);
+    else Loop::run(smem, acc);
   }
   __device__ __forceinline__ void run_idle(char* smem) {
     of_tile = turn;
@@ -190,9 +242,11 @@ struct RowScaled : Loop {
     }
   }
 };
-typedef RowScaled<TileGemm<I8, 11, 2, true, SlabRing>> Rows256;
+typedef RowScaled<TileGemm<I8, 11, 2, true, SlabRing>> Rows256;            // counted: the two stores of a token's partials,
+typedef RowScaled<TileGemm<I8, 11, 8, true, SlabRing>> Rows256Stored;      // ... the stores of the tile's last two column blocks
 typedef RowScaled<TileGemmSmall<I8, Shape128, 2, 2>> Rows128;
-typedef RowScaled<TileGemmSmall<I8, Shape64x64, 4, 2>> Rows64;
+typedef RowScaled<TileGemmRing<Shape64x64, 4, 2>> Rows64;
+typedef RowScaled<TileGemmRing<Shape64x64, 8, 1>> Rows64Deep;              // as much of W on its way where a CU has one tile
 
 template <typename G>
 __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_partials(FwdArgs a, RowHead x) {
@@ -209,6 +263,7 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_partial
 struct RowLogitsArgs {
   RowHead x;
   int64_t N, d, V;
+  int64_t v_first, v_end;  // rows of W of this launch; v_first a multiple of 256
   int tiles_v, tiles_t;
   void* z;                 // [N][V]
 };
@@ -224,12 +279,12 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_logits(
   const int last_row = (int)a.N - 1;
   auto setup = [&](const LogitsTile& t) {
     const int lane = threadIdx.x & 63, wave = wave_id(), t0 = t.tt * S::BN;
-    const int64_t v0 = (int64_t)t.tv * S::BM;
+    const int64_t v0 = a.v_first + (int64_t)t.tv * S::BM;
     int grow[decltype(g.lb)::ITERS];
 #pragma unroll
     for (int it = 0; it < decltype(g.lb)::ITERS; ++it)
       grow[it] = min(t0 + decltype(g.lb)::template lane_tile_row<false>(it, wave, lane, S::NB), last_row);
-    g.template setup_gathered<false>(a.x.W + v0 * a.d, a.d, (int)min((int64_t)S::BM, a.V - v0), a.x.H, a.d,
+    g.template setup_gathered<false>(a.x.W + v0 * a.d, a.d, (int)min((int64_t)S::BM, a.v_end - v0), a.x.H, a.d,
                                      (int)min((int64_t)S::BN, a.N - t0), a.d, grow, a.N,
                                      a.N <= TURN_COLUMNS * S::BN ? t.tv / PATCH_ROWS_LOGITS : 0);
     g.set_scale_rows(v0, min(t0 + wave % G::PIECES * 64 + lane, last_row));
@@ -239,11 +294,13 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_logits(
   setup(cur);
 #pragma unroll
   for (int q = 0; q < G::FIRST_PARTS; ++q) g.issue_first(smem, q);
+  bool counted = false;
   while (true) {
     f32x4_t acc[S::MB][S::NB];
-    const int64_t v0 = (int64_t)cur.tv * S::BM, t0 = (int64_t)cur.tt * S::BN;
-    const int rowsV = (int)min((int64_t)S::BM, a.V - v0), rowsT = (int)min((int64_t)S::BN, a.N - t0);
-    run_tile<G, S::NB>(g, smem, acc, S::wave_col(wave_id()) * S::WAVE_N >= rowsT);
+    const int64_t v0 = a.v_first + (int64_t)cur.tv * S::BM, t0 = (int64_t)cur.tt * S::BN;
+    const int rowsV = (int)min((int64_t)S::BM, a.v_end - v0), rowsT = (int)min((int64_t)S::BN, a.N - t0);
+    run_tile<G, S::NB>(g, smem, acc, S::wave_col(wave_id()) * S::WAVE_N >= rowsT, counted);
+    counted = rowsV == S::BM && rowsT == S::BN;      // every lane stores
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                    // as in fwd_tiles
     const LanePos<S> lp(tid);
@@ -259,7 +316,7 @@ __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_logits(
     }
     LLAMARL_FENCE();
     g.finish(acc, lp);
-    TileStore<S, Out>::run(static_cast<Out*>(a.z) + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT, smem + G::LDS_BYTES, [&](int j) {
+    TileStore<S, Out, true>::run(static_cast<Out*>(a.z) + t0 * a.V + v0, a.V, acc, lp, rowsV, rowsT, smem + G::LDS_BYTES, [&](int j) {
       if (!last && 2 + j < G::FIRST_PARTS) g.issue_first(smem, 2 + j);
     });
     if (last) break;

@@ -358,17 +358,40 @@ LLAMARL_RULE int64_t block_partials(int64_t N, int64_t V) {
 
 // ---- heads in 8-bit integers (row_kernels.h) --------------------------------------------------------------------------------
 // Which kernel a product of N tokens with V rows of W takes.
-enum RowTile { ROW_DIRECT, ROW_64, ROW_128, ROW_256 };
+enum RowTile { ROW_DIRECT, ROW_64_DEEP, ROW_64, ROW_128, ROW_256 };
 constexpr int64_t ROW_64_TILES = 256;
 LLAMARL_RULE RowTile row_tile(int64_t N, int64_t V) {
   if (N <= DIRECT_TOKENS) return ROW_DIRECT;
-  if (tile_count(N, V, 128) < ROW_64_TILES) return ROW_64;
+  if (tile_count(N, V, 128) < ROW_64_TILES) return tile_count(N, V, 64) <= 256 ? ROW_64_DEEP : ROW_64;
   return N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? ROW_256 : ROW_128;
 }
 // rows of W that a tile of partials has
 LLAMARL_RULE int row_tile_rows(RowTile t, int64_t d) {
   const int direct = DIRECT_WAVES / direct_parts(d) * 16;
-  return t == ROW_256 ? 256 : t == ROW_128 ? 128 : t == ROW_64 ? 64 : direct < 64 ? direct : 64;
+  return t == ROW_256 ? 256 : t == ROW_128 ? 128 : t >= ROW_64_DEEP ? 64 : direct < 64 ? direct : 64;
+}
+// Logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own, by what
+// rounds of the grid cost (block_logits).
+struct RowLogits {
+  RowTile tile;
+  int64_t rows;
+  RowTile rest;
+};
+LLAMARL_RULE RowLogits row_logits(int64_t N, int64_t V, int64_t d) {
+  const RowTile t = row_tile(N, V);
+  if (N <= FEW_TOKENS || t < ROW_128) return {t, V, t};
+  const int64_t tiles_t = (N + 255) / 256, tiles = tile_count(N, V, 256), rows = tiles / 256 * 256 / tiles_t * 256;
+  const int64_t round = (14000 + 25 * d / 2) * (4 * tiles_t - ((N - 1) % 256 < 128)) / (4 * tiles_t);
+  RowLogits best = {ROW_128, V, ROW_128};
+  int64_t cost = block_cost_128(N, V, d);
+  const int64_t whole = (tiles + 255) / 256 * round;
+  if (whole < cost) {
+    best.tile = ROW_256;
+    cost = whole;
+  }
+  if (rows > 0 && rows < V && tiles / 256 * round + block_cost_128(N, V - rows, d) + 3000 < cost)
+    best = {ROW_256, rows, tile_count(N, V - rows, 128) < ROW_64_TILES ? ROW_64 : ROW_128};
+  return best;
 }
 // Floats of a plane of partials that serves any call of up to N tokens and V rows, see block_partials.
 LLAMARL_RULE int64_t row_partials(int64_t N, int64_t V) {
