@@ -760,12 +760,15 @@ PyObject* rms_norm_bwd(PyObject* const* a) {
   at::Tensor dw, ws;
   if (wanted) {
     dw = empty(r.x, {r.d}, code < 0 ? r.w.scalar_type() : code == LLAMARL_BF16 ? at::kBFloat16 : at::kFloat);
-    ws = workspace(a[7], llamarl_rms_norm_bwd_workspace_bytes(r.N, r.d), r.x);
-    on_device_of(ws.is_cuda() ? ws : at::Tensor(), r.x, "ws", "the rows");
+    const size_t need = llamarl_rms_norm_bwd_workspace_bytes(r.N, r.d);
+    if (need > 0 || a[7] != Py_None) {
+      ws = workspace(a[7], need, r.x);
+      on_device_of(ws.is_cuda() ? ws : at::Tensor(), r.x, "ws", "the rows");
+    }
   }
   check(unlocked([&] {
     return llamarl_rms_norm_bwd(ptr(dh), ptr(r.x), ptr(r.w), ptr<float>(rstd), ptr(dsum), r.N, r.d, r.dt, r.w_dt, ptr(dx), ptr(dw),
-                                wanted ? dtype_code(dw) : LLAMARL_F32, ptr(ws), wanted ? (size_t)ws.nbytes() : 0, st.handle);
+                                wanted ? dtype_code(dw) : LLAMARL_F32, ptr(ws), ws.defined() ? (size_t)ws.nbytes() : 0, st.handle);
   }));
   st.returns(dx);
   if (wanted) {

@@ -7,13 +7,25 @@ template <int TH_, int UNITS_>
 struct RowShape {
   static constexpr int TH = TH_, UNITS = UNITS_;
 };
-// f(RowShape) for rows of d entries, units of eight: a wavefront where four units each hold a row, else 256 or 1024 threads.
+// f(RowShape) for rows of d entries: a wavefront a row up to 1024, then as many threads as have units of eight.  Forward of 16384 x 4096 bf16 rows on 256
+// threads with two units each / 512 with one 91.9 / 89.9 us, 1900 x 8192 (four / 1024 with one) 20.8 / 19.7, 16384 x 2048 (64 with four / 256) 44.0 / 39.9.
 template <typename F>
 auto with_row_shape(int64_t d, F&& f) {
   const int64_t units = (d + OPT_ITEMS - 1) / OPT_ITEMS;
   if (units <= 64) return f(RowShape<64, 1>());
   if (units <= 128) return f(RowShape<64, 2>());
-  if (units <= 256) return f(RowShape<64, 4>());
+  if (units <= 256) return f(RowShape<256, 1>());
+  if (units <= 512) return f(RowShape<512, 1>());
+  if (units <= 1024) return f(RowShape<1024, 1>());
+  return f(RowShape<1024, 2>());
+}
+// ... of quantise_rows, which holds less of a row: 16384 x 4096 on 256 threads / 512 29.2 / 32.3 us, 1900 x 8192 on 256 / 1024 8.3 / 9.9.
+template <typename F>
+auto with_quantise_shape(int64_t d, F&& f) {
+  const int64_t units = (d + OPT_ITEMS - 1) / OPT_ITEMS;
+  if (units <= 64) return f(RowShape<64, 1>());
+  if (units <= 128) return f(RowShape<64, 2>());
+  if (units <= 256) return f(RowShape<256, 1>());
   if (units <= 512) return f(RowShape<256, 2>());
   if (units <= 1024) return f(RowShape<256, 4>());
   return f(RowShape<1024, 2>());
@@ -37,7 +49,11 @@ llamarl_status check_norm(int64_t N, int64_t d, llamarl_dtype dt, llamarl_dtype 
   if (!aligned16(w)) return fail(LLAMARL_ERR_INVALID_ARG, "weight must be 16-byte aligned");
   return check_row_launch(N, d);
 }
-int64_t norm_bwd_blocks(int64_t N, int64_t d) { return std::min<int64_t>((N + rows_each(d) - 1) / rows_each(d), NORM_BWD_BLOCKS); }
+// workgroups, and rows of partial sums; none for few rows, whose columns are summed up as they are
+int64_t norm_bwd_blocks(int64_t N, int64_t d) {
+  return std::min<int64_t>((N + rows_each(d) - 1) / rows_each(d), row_threads(d) == 1024 ? NORM_BWD_BLOCKS / 2 : NORM_BWD_BLOCKS);
+}
+bool norm_columns(int64_t N) { return N <= NORM_FEW_ROWS; }
 
 template <typename T, int OUT>
 llamarl_status launch_norm(const NormArgs& a, hipStream_t st) {
@@ -56,10 +72,11 @@ llamarl_status launch_norm_out(const NormArgs& a, llamarl_norm_out out, hipStrea
          : out == LLAMARL_NORM_E4M3_BLOCKS ? launch_norm<T, OUT_BLOCKS>(a, st) : launch_norm<T, OUT_ROWS>(a, st);
 }
 template <typename T>
-void launch_norm_bwd(const NormBwdArgs& a, int64_t blocks, hipStream_t st) {
+void launch_norm_bwd(const NormBwdArgs& a, hipStream_t st) {
+  const int columns = a.dw ? (a.d + NORM_COLUMNS - 1) / NORM_COLUMNS : 0;
   with_row_shape(a.d, [&](auto s) {
     constexpr int TH = decltype(s)::TH;
-    k_rms_norm_bwd<T, TH, decltype(s)::UNITS><<<dim3((unsigned)blocks), dim3(NORM_THREADS_OF<TH>), 0, st>>>(a);
+    k_rms_norm_bwd<T, TH, decltype(s)::UNITS><<<dim3((unsigned)(a.row_blocks + columns)), dim3(NORM_THREADS_OF<TH>), 0, st>>>(a);
     return 0;
   });
 }
@@ -93,7 +110,7 @@ llamarl_status llamarl_rms_norm(const void* x, const void* residual, const void*
 }
 
 size_t llamarl_rms_norm_bwd_workspace_bytes(int64_t N, int64_t d) {
-  return N <= 0 || d <= 0 || d > NORM_MOST_COLS ? 0 : (size_t)(norm_bwd_blocks(N, d) * d * 4);
+  return N <= 0 || d <= 0 || d > NORM_MOST_COLS || norm_columns(N) ? 0 : (size_t)(norm_bwd_blocks(N, d) * d * 4);
 }
 
 llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* weight, const float* rstd, const void* dsum, int64_t N,
@@ -106,22 +123,24 @@ llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* w
   if (!aligned16(dh) || !aligned16(s) || !aligned16(dsum) || !aligned16(dx)) return fail(LLAMARL_ERR_INVALID_ARG, "dh, s, dsum and dx must be 16-byte aligned");
   if (!aligned_to(rstd, 4) || !aligned_to(dweight, esize(dw_dt))) return fail(LLAMARL_ERR_INVALID_ARG, "misaligned rstd or dweight");
   const size_t need = llamarl_rms_norm_bwd_workspace_bytes(N, d);
-  if (dweight != nullptr) {
+  if (dweight != nullptr && need > 0) {
     if (!ws || ws_bytes < need)
       return fail(LLAMARL_ERR_WORKSPACE, "workspace of %zu bytes given, %zu needed", ws ? ws_bytes : (size_t)0, need);
     if (!aligned16(ws)) return fail(LLAMARL_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
   }
   const int64_t bytes = N * d * (int64_t)esize(dt);
-  if (any_overlap({{dx, bytes}, {dweight, d * (int64_t)esize(dw_dt)}, {dweight ? ws : nullptr, (int64_t)need}},
+  if (any_overlap({{dx, bytes}, {dweight, d * (int64_t)esize(dw_dt)}, {dweight && need > 0 ? ws : nullptr, (int64_t)need}},
                   {{dh, bytes}, {s, bytes}, {dsum, bytes}, {weight, d * (int64_t)esize(w_dt)}, {rstd, N * 4}}))
     return fail(LLAMARL_ERR_INVALID_ARG, "outputs and workspace must not overlap another array");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const int64_t blocks = norm_bwd_blocks(N, d);
-  const NormBwdArgs a = {dh, s, weight, rstd, dsum, N, (int)d, w_dt == LLAMARL_BF16, dx, dweight ? static_cast<float*>(ws) : nullptr};
-  if (dt == LLAMARL_BF16) launch_norm_bwd<uint16_t>(a, blocks, st);
-  else launch_norm_bwd<float>(a, blocks, st);
+  const bool columns = dweight != nullptr && norm_columns(N);
+  const NormBwdArgs a = {dh, s, weight, rstd, dsum, N, (int)d, w_dt == LLAMARL_BF16, dx, dweight && !columns ? static_cast<float*>(ws) : nullptr,
+                         (int)blocks, columns ? dweight : nullptr, dw_dt == LLAMARL_BF16};
+  if (dt == LLAMARL_BF16) launch_norm_bwd<uint16_t>(a, st);
+  else launch_norm_bwd<float>(a, st);
   HIP_TRY(hipGetLastError());
-  if (dweight == nullptr) return LLAMARL_OK;
+  if (a.part == nullptr) return LLAMARL_OK;
   k_norm_dw<<<dim3((unsigned)((d + NORM_DW_COLS - 1) / NORM_DW_COLS)), dim3(NORM_DW_COLS * NORM_DW_SLICES), 0, st>>>(
       a.part, (int)blocks, (int)d, dweight, dw_dt == LLAMARL_BF16);
   HIP_TRY(hipGetLastError());

@@ -206,17 +206,54 @@ struct NormBwdArgs {
   int d;
   int w_bf16;
   void* dx;
-  float* part;             // [gridDim.x][d]; null: dw is not asked for
+  float* part;             // [row_blocks][d]; null: dw is not asked for, or
+  int row_blocks;
+  void* dw;                // ... the workgroups behind the row_blocks sum up a few columns each
+  int dw_bf16;
 };
-// Workgroups of 256 (1024) threads walk over the rows, TH threads a row, the columns' share of dw in registers; its sums of a workgroup meet in LDS.
-constexpr int NORM_BWD_BLOCKS = 1024;
+// dw of few rows: NORM_COLUMNS columns a workgroup, dh and s read a second time (from L2), where partial sums would take a launch more: 333 x 520
+// 3.8 + 3.1 us.
+constexpr int64_t NORM_FEW_ROWS = 512;
+constexpr int NORM_COLUMNS = 64;
+template <typename T, int THREADS>
+__device__ __forceinline__ void norm_columns(const NormBwdArgs& a, int block) {
+  constexpr int LANES = NORM_COLUMNS / OPT_ITEMS, SLICES = THREADS / LANES;
+  __shared__ float s_dw[SLICES][NORM_COLUMNS + 1];
+  const int slice = threadIdx.x / LANES, col = block * NORM_COLUMNS + threadIdx.x % LANES * OPT_ITEMS;
+  float dw[OPT_ITEMS] = {};
+#pragma unroll 4
+  for (int64_t row = slice; row < a.N; row += SLICES) {
+    Raw8<T> g, x;
+    load_unit(g, a.dh, row * a.d + col, a.d - col);
+    load_unit(x, a.s, row * a.d + col, a.d - col);
+    const float r = a.rstd[row];
+    float dh[OPT_ITEMS], s[OPT_ITEMS];
+    g.get(dh);
+    x.get(s);
+#pragma unroll
+    for (int e = 0; e < OPT_ITEMS; ++e) dw[e] = fmaf(dh[e], s[e] * r, dw[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < OPT_ITEMS; ++e) s_dw[slice][threadIdx.x % LANES * OPT_ITEMS + e] = dw[e];
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c >= NORM_COLUMNS || block * NORM_COLUMNS + c >= a.d) return;
+  float t = 0.f;
+  for (int q = 0; q < SLICES; ++q) t += s_dw[q][c];
+  if (a.dw_bf16) static_cast<uint16_t*>(a.dw)[block * NORM_COLUMNS + c] = float_to_bf16_bits(t);
+  else static_cast<float*>(a.dw)[block * NORM_COLUMNS + c] = t;
+}
+// Workgroups of 256 to 1024 threads walk over the rows, TH threads a row, the columns' share of dw in registers; its sums of a workgroup meet in LDS.
+// Two workgroups a CU (one of 1024 threads): what a workgroup leaves of dw is written and read again, 4 d bytes each.
+constexpr int NORM_BWD_BLOCKS = 512;
 template <typename T, int TH, int UNITS>
 __global__ __launch_bounds__(NORM_THREADS_OF<TH>) void k_rms_norm_bwd(NormBwdArgs a) {
   constexpr int ROWS = NORM_THREADS_OF<TH> / TH, WAVES = TH / 64;
   __shared__ float s_dot[2][WAVES];
   __shared__ float s_dw[ROWS > 1 ? ROWS * TH * UNITS * OPT_ITEMS : 1];
+  if ((int)blockIdx.x >= a.row_blocks) return norm_columns<T, NORM_THREADS_OF<TH>>(a, blockIdx.x - a.row_blocks);
   const int tid = threadIdx.x % TH, lane = threadIdx.x & 63, wave = tid / 64, own = ROWS > 1 ? wave_id() : 0;
-  constexpr bool ROOMY = TH < 1024;                  // 1024 threads have 128 registers each: w comes from L2 row by row, dsum late
+  constexpr bool ROOMY = TH * UNITS < 2048;                // 1024 threads have 128 registers each: w comes from L2 row by row, dsum late
   float w[UNITS][OPT_ITEMS], dw[UNITS][OPT_ITEMS];
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
@@ -227,36 +264,52 @@ __global__ __launch_bounds__(NORM_THREADS_OF<TH>) void k_rms_norm_bwd(NormBwdArg
   }
   const float inv_d = 1.f / (float)a.d;
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + own; row < a.N; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
-    const int64_t first = row * a.d;
-    Raw8<T> g[UNITS], x[UNITS], u[UNITS];
+  Raw8<T> g[UNITS], x[UNITS], u[UNITS];
+  float r = 0.f;
+  const int64_t stride = (int64_t)a.row_blocks * ROWS;
+  auto load_sums = [&](int64_t row) {
+    if (a.dsum != nullptr) {                         // uniform
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) load_unit(u[i], a.dsum, row * a.d + (i * TH + tid) * OPT_ITEMS, a.d - (i * TH + tid) * OPT_ITEMS);
+    }
+  };
+  auto load_row = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       const int col = (i * TH + tid) * OPT_ITEMS;
-      load_unit(g[i], a.dh, first + col, a.d - col);
-      load_unit(x[i], a.s, first + col, a.d - col);
+      load_unit(g[i], a.dh, row * a.d + col, a.d - col);
+      load_unit(x[i], a.s, row * a.d + col, a.d - col);
     }
-    const float r = a.rstd[row];
-    if (ROOMY && a.dsum != nullptr) {                // uniform
-#pragma unroll
-      for (int i = 0; i < UNITS; ++i) {
-        const int col = (i * TH + tid) * OPT_ITEMS;
-        load_unit(u[i], a.dsum, first + col, a.d - col);
-      }
-    }
+    r = a.rstd[row];
+    if constexpr (ROOMY) load_sums(row);
+  };
+  int64_t row = (int64_t)blockIdx.x * ROWS + own;
+  if (ROOMY && row < a.N) load_row(row);
+  for (; row < a.N; row += stride, turn ^= 1) {
+    const int64_t first = row * a.d;
+    if constexpr (!ROOMY) load_row(row);
+    float dh[UNITS][OPT_ITEMS], s[UNITS][OPT_ITEMS];
+    Raw8<T> more[UNITS];
+    const float rs = r;
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
+      g[i].get(dh[i]);
+      x[i].get(s[i]);
+      if constexpr (ROOMY) more[i] = u[i];
+    }
+    if constexpr (ROOMY) {                           // the next row on its way while this one is reduced and stored
+      if (row + stride < a.N) load_row(row + stride);
+    }
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
       const int col = (i * TH + tid) * OPT_ITEMS;
-      float dh[OPT_ITEMS], s[OPT_ITEMS];
       if constexpr (!ROOMY) load_weights(a.w, a.w_bf16, col, a.d - col, w[i]);
-      g[i].get(dh);
-      x[i].get(s);
 #pragma unroll
       for (int e = 0; e < OPT_ITEMS; ++e) {
-        const float n = s[e] * r;
-        dot = fmaf(dh[e] * w[i][e], n, dot);
-        dw[i][e] = fmaf(dh[e], n, dw[i][e]);
+        const float n = s[i][e] * rs;
+        dot = fmaf(dh[i][e] * w[i][e], n, dot);
+        dw[i][e] = fmaf(dh[i][e], n, dw[i][e]);
       }
     }
     dot = wave_sum(dot);
@@ -268,21 +321,20 @@ __global__ __launch_bounds__(NORM_THREADS_OF<TH>) void k_rms_norm_bwd(NormBwdArg
       for (int q = 1; q < WAVES; ++q) dot += s_dot[turn][q];
     }
     const float mean = dot * inv_d;
+    if constexpr (!ROOMY) load_sums(row);
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       const int col = (i * TH + tid) * OPT_ITEMS;
-      float dh[OPT_ITEMS], s[OPT_ITEMS], o[OPT_ITEMS];
+      float o[OPT_ITEMS];
       if constexpr (!ROOMY) {
         load_weights(a.w, a.w_bf16, col, a.d - col, w[i]);
-        if (a.dsum != nullptr) load_unit(u[i], a.dsum, first + col, a.d - col);
+        more[i] = u[i];
       }
-      g[i].get(dh);
-      x[i].get(s);
 #pragma unroll
-      for (int e = 0; e < OPT_ITEMS; ++e) o[e] = r * fmaf(-(s[e] * r), mean, dh[e] * w[i][e]);
+      for (int e = 0; e < OPT_ITEMS; ++e) o[e] = rs * fmaf(-(s[i][e] * rs), mean, dh[i][e] * w[i][e]);
       if (a.dsum != nullptr) {
         float t[OPT_ITEMS];
-        u[i].get(t);
+        more[i].get(t);
 #pragma unroll
         for (int e = 0; e < OPT_ITEMS; ++e) o[e] += t[e];
       }

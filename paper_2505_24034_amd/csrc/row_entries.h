@@ -77,7 +77,7 @@ void launch_quantise_int8(const QuantiseRowsArgs& a, hipStream_t st) {
     k_quantise_int8<T, 1024, 0><<<dim3((unsigned)a.rows), dim3(1024), 0, st>>>(a);
     return;
   }
-  with_row_shape(a.cols, [&](auto s) {
+  with_quantise_shape(a.cols, [&](auto s) {
     constexpr int TH = decltype(s)::TH;
     const int64_t per = rows_each(a.cols);
     k_quantise_int8<T, TH, decltype(s)::UNITS><<<dim3((unsigned)((a.rows + per - 1) / per)), dim3(NORM_THREADS_OF<TH>), 0, st>>>(a);

@@ -69,8 +69,8 @@ def test_workspace_of_the_largest_call_serves_smaller_ones():
             assert b >= last and b >= L.logprobs_rows_workspace_bytes(N, max(1, V - 77))
             last = b
     for d in (8, 2048, 4096, 16384):
-        sizes = [L.rms_norm_bwd_workspace_bytes(N, d) for N in (1, 2, 5, 100, 1024, 5000, 100000)]
-        assert sizes == sorted(sizes) and sizes[0] > 0
+        sizes = [L.rms_norm_bwd_workspace_bytes(N, d) for N in (1, 2, 5, 100, 512, 513, 1024, 5000, 100000)]
+        assert sizes == sorted(sizes) and sizes[5] > 0
     last = 0
     for B, K, V in ((1, 0, 1), (1, 1, 1), (2, 1, 8192), (2, 1, 8193), (2, 9, 8193), (300, 9, 100000)):
         b = L.verify_drafts_workspace_bytes(B, K, V)
@@ -105,9 +105,10 @@ def test_rms_norm(clib):
 
 @no_gpu_only
 def test_rms_norm_bwd(clib):
-    need = L.rms_norm_bwd_workspace_bytes(10, 64)
+    need = L.rms_norm_bwd_workspace_bytes(600, 64)
+    assert need > 0 and L.rms_norm_bwd_workspace_bytes(512, 64) == 0      # few rows need none
 
-    def call(dh=A, s=2 * A, w=3 * A, rstd=4 * A, dsum=5 * A, N=10, d=64, dt=L.BF16, w_dt=L.BF16, dx=6 * A, dw=7 * A, dw_dt=L.F32, ws=8 * A, nbytes=need):
+    def call(dh=A, s=2 * A, w=3 * A, rstd=4 * A, dsum=5 * A, N=600, d=64, dt=L.BF16, w_dt=L.BF16, dx=6 * A, dw=7 * A, dw_dt=L.F32, ws=8 * A, nbytes=need):
         return clib.llamarl_rms_norm_bwd(vp(dh), vp(s), vp(w), vp(rstd), vp(dsum), N, d, dt, w_dt, vp(dx), vp(dw), dw_dt, vp(ws), nbytes, None)
 
     for bad in (dict(dh=None), dict(s=None), dict(w=None), dict(rstd=None), dict(dx=None), dict(N=-1), dict(d=0), dict(dt=9), dict(w_dt=2), dict(dw_dt=2),

@@ -13,7 +13,7 @@ from operator_util import f64
 pytestmark = pytest.mark.gpu
 EPS = 1e-5
 SHAPES = [(1, 8), (4, 16), (5, 520), (3, 1032), (2, 1544), (7, 2048), (3, 2056), (1, 4096), (2, 5000), (5, 8192), (2, 8200), (3, 16384),
-          (333, 528), (4100, 64)]
+          (333, 528), (512, 1032), (513, 1032), (1100, 520), (600, 2056), (520, 4104), (514, 8208), (4100, 64)]
 
 
 def _rows(N, d, dtype, seed, w_dtype=None):
@@ -54,7 +54,7 @@ def test_forward_and_backward(lib, N, d, dtype):
         assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
 
 
-@pytest.mark.parametrize("N,d", [(1, 4), (3, 516), (5, 1028), (2, 4100), (9, 260)])
+@pytest.mark.parametrize("N,d", [(1, 4), (3, 516), (5, 1028), (2, 4100), (9, 260), (700, 1028), (530, 4100), (520, 12)])
 def test_fp32_rows_of_four(lib, N, d):
     x, res, w, dh, _ = _rows(N, d, torch.float32, d, torch.bfloat16 if N % 2 else torch.float32)
     h, s, rstd = lib.rms_norm(x, w, EPS, residual=res)
