@@ -876,17 +876,13 @@ PyObject* block_logits_plan(PyObject* const* a) {
   return Py_BuildValue("iLi", (int)p.tile, (long long)p.rows, (int)p.rest);
 }
 
-// N, V, d: kernel (RowTile) of a product with a head in 8-bit integers, rows of its tiles of partials, floats of their planes
+// N, V, d, log-probs: kernel (RowTile) of the first rows of W, how many, kernel of the rest; rows of partials of the two, floats of a plane of them
 PyObject* row_plan(PyObject* const* a) {
-  const int64_t N = integer(a[0]), V = integer(a[1]);
-  const llamarl::RowTile t = llamarl::row_tile(N, V);
-  return Py_BuildValue("iiL", (int)t, llamarl::row_tile_rows(t, integer(a[2])), (long long)llamarl::row_partials(N, V));
-}
-
-// (N, V, d) -> kernel of the first rows of W, how many, kernel of the rest: logits of a head in 8-bit integers
-PyObject* row_logits_plan(PyObject* const* a) {
-  const llamarl::RowLogits p = llamarl::row_logits(integer(a[0]), integer(a[1]), integer(a[2]));
-  return Py_BuildValue("iLi", (int)p.tile, (long long)p.rows, (int)p.rest);
+  const int64_t N = integer(a[0]), V = integer(a[1]), d = integer(a[2]);
+  const llamarl::RowPlan p = llamarl::row_plan(N, V, d, integer(a[3]) != 0);
+  const int first = llamarl::row_tile_rows(p.tile, d), rest = llamarl::row_tile_rows(p.rest, d);
+  return Py_BuildValue("iLiLL", (int)p.tile, (long long)p.rows, (int)p.rest, (long long)((p.rows + first - 1) / first + (V - p.rows + rest - 1) / rest),
+                       (long long)llamarl::row_partials(N, V));
 }
 
 template <PyObject* (*F)(PyObject* const*), int NARGS>
@@ -917,7 +913,7 @@ PyMethodDef g_methods[] = {
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
     ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
     ENTRY(token_logprobs_blocks, 8), ENTRY(quantise_rows, 2), ENTRY(logits_rows, 7), ENTRY(token_logprobs_rows, 8), ENTRY(rms_norm, 6),
-    ENTRY(rms_norm_bwd, 9), ENTRY(verify_drafts, 8), ENTRY(row_plan, 3), ENTRY(row_logits_plan, 3), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(rms_norm_bwd, 9), ENTRY(verify_drafts, 8), ENTRY(row_plan, 4), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

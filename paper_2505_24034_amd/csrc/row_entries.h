@@ -58,8 +58,7 @@ llamarl_status launch_row_logits(RowLogitsArgs a, hipStream_t st) {
 }
 template <typename Out>
 llamarl_status launch_row_tiles(const RowLogitsArgs& a, RowTile t, hipStream_t st) {
-  return (t == ROW_256 ? launch_row_logits<Rows256Stored, Out> : t == ROW_128 ? launch_row_logits<Rows128, Out>
-          : t == ROW_64 ? launch_row_logits<Rows64, Out> : launch_row_logits<Rows64Deep, Out>)(a, st);
+  return (t == ROW_256 ? launch_row_logits<Rows256Stored, Out> : t == ROW_128 ? launch_row_logits<Rows128, Out> : launch_row_logits<Rows64, Out>)(a, st);
 }
 template <typename G>
 llamarl_status launch_row_partials(const FwdArgs& a, const RowHead& x, hipStream_t st) {
@@ -118,7 +117,7 @@ llamarl_status llamarl_logits_rows(const int8_t* H, const float* H_scale, const 
   if (any_overlap({{z, N * V * (int64_t)esize(z_dt)}}, {{H, N * d}, {H_scale, N * 4}, {W, V * d}, {W_scale, V * 4}}))
     return fail(LLAMARL_ERR_INVALID_ARG, "z must not overlap an operand");
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const RowLogits plan = row_logits(N, V, d);
+  const RowPlan plan = row_plan(N, V, d, false);
   if (plan.tile == ROW_DIRECT) {
     RowFewArgs f = {};
     f.x = x;
@@ -156,11 +155,12 @@ llamarl_status llamarl_token_logprobs_rows(const int8_t* H, const float* H_scale
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   char* base = reinterpret_cast<char*>(ws);
   int32_t *rows = reinterpret_cast<int32_t*>(base + w.off_rows), *n_act = reinterpret_cast<int32_t*>(base + w.off_nact);
-  const RowTile tile = row_tile(N, V);
-  const int tile_rows = row_tile_rows(tile, d);
+  const RowPlan plan = row_plan(N, V, d, true);
+  const int tile_rows = row_tile_rows(plan.tile, d), rest_rows = row_tile_rows(plan.rest, d);
+  const int tiles = (int)((plan.rows + tile_rows - 1) / tile_rows), rest = (int)((V - plan.rows + rest_rows - 1) / rest_rows);
   FwdArgs a = {};
   a.H = H; a.W = W; a.targets = targets; a.N = N; a.d = d; a.V = V;
-  a.tiles_v = (int)((V + tile_rows - 1) / tile_rows);
+  a.tiles_v = tiles + rest;
   a.n_pad = w.n_pad;
   if (a.tiles_v * w.n_pad > w.plane) return fail(LLAMARL_ERR_WORKSPACE, "partials of %d tiles do not fit", a.tiles_v);      // a mistake in the rules
   a.part_m = reinterpret_cast<float*>(base + w.off_m);
@@ -170,14 +170,22 @@ llamarl_status llamarl_token_logprobs_rows(const int8_t* H, const float* H_scale
   k_compact_rows<<<dim3((unsigned)compact_blocks(N)), dim3(COMPACT_THREADS), 0, st>>>(
       compact_args({0, mask, targets, nullptr, V, N, 0, rows, n_act, logp, lse, nullptr, 0.f, nullptr, nullptr}));
   HIP_TRY(hipGetLastError());
-  if (tile == ROW_DIRECT) {
+  if (plan.tile == ROW_DIRECT) {
     RowFewArgs f = {};
     f.x = x;
     f.few.N = N; f.few.d = d; f.few.V = V; f.few.f = a;
     s = launch_row_direct<void>(f, st);
   } else {
-    s = (tile == ROW_256 ? launch_row_partials<Rows256> : tile == ROW_128 ? launch_row_partials<Rows128>
-         : tile == ROW_64 ? launch_row_partials<Rows64> : launch_row_partials<Rows64Deep>)(a, x, st);
+    // rows [first, first + count) of W, their partials from tile `at` on
+    const auto launch = [&](RowTile t, int64_t first, int64_t count, int at, int n) {
+      FwdArgs p = a;
+      p.W = W + first * d; p.V = count; p.v_off = first; p.tiles_v = n;
+      p.part_m += at * w.n_pad; p.part_s += at * w.n_pad;
+      const RowHead y = {H, W + first * d, H_scale, W_scale + first};
+      return (t == ROW_256 ? launch_row_partials<Rows256> : t == ROW_128 ? launch_row_partials<Rows128> : launch_row_partials<Rows64>)(p, y, st);
+    };
+    s = launch(plan.tile, 0, plan.rows, 0, tiles);
+    if (s == LLAMARL_OK && rest > 0) s = launch(plan.rest, plan.rows, V - plan.rows, tiles, rest);
   }
   if (s != LLAMARL_OK) return s;
   return launch_merge(a, logp, lse, nullptr, 0, StoredTarget(), st);

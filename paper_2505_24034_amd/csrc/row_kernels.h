@@ -131,7 +131,9 @@ struct RowHead {
   const float* h_scale;
   const float* w_scale;
 };
-// TileGemmSmall with its slabs taken round a ring (SlabRing), for W that streams from memory: workgroups start at slabs of their own.
+// TileGemmSmall with its slabs taken round a ring (SlabRing), for W that streams from memory: workgroups start at slabs of their own.  From slab 0 / round a
+// ring, us, logits of (64, 128256, 4096) 131 / 108, (100, 128256, 4096) 134 / 114, (64, 50000, 8192) 90 / 82, (48, 16032, 8192) on 64 x 64 31.0 / 26.  Eight slabs of
+// 64 x 64 resident instead of four: (16, 16032, 8192) 24.8 for 24.2, (33, 128256, 4096) 117 for 117.
 template <typename S_, int NSTAGE, int GROUPS_PER_CU_>
 struct TileGemmRing : TileGemmSmall<I8, S_, NSTAGE, GROUPS_PER_CU_> {
   typedef TileGemmSmall<I8, S_, NSTAGE, GROUPS_PER_CU_> Base;
@@ -244,9 +246,8 @@ struct RowScaled : Loop {
 };
 typedef RowScaled<TileGemm<I8, 11, 2, true, SlabRing>> Rows256;            // counted: the two stores of a token's partials,
 typedef RowScaled<TileGemm<I8, 11, 8, true, SlabRing>> Rows256Stored;      // ... the stores of the tile's last two column blocks
-typedef RowScaled<TileGemmSmall<I8, Shape128, 2, 2>> Rows128;
+typedef RowScaled<TileGemmRing<Shape128, 2, 2>> Rows128;
 typedef RowScaled<TileGemmRing<Shape64x64, 4, 2>> Rows64;
-typedef RowScaled<TileGemmRing<Shape64x64, 8, 1>> Rows64Deep;              // as much of W on its way where a CU has one tile
 
 template <typename G>
 __global__ __launch_bounds__(G::Shape::THREADS, MIN_WAVES<G>) void k_row_partials(FwdArgs a, RowHead x) {

@@ -357,48 +357,69 @@ LLAMARL_RULE int64_t block_partials(int64_t N, int64_t V) {
 }
 
 // ---- heads in 8-bit integers (row_kernels.h) --------------------------------------------------------------------------------
-// Which kernel a product of N tokens with V rows of W takes.
-enum RowTile { ROW_DIRECT, ROW_64_DEEP, ROW_64, ROW_128, ROW_256 };
-constexpr int64_t ROW_64_TILES = 256;
-LLAMARL_RULE RowTile row_tile(int64_t N, int64_t V) {
-  if (N <= DIRECT_TOKENS) return ROW_DIRECT;
-  if (tile_count(N, V, 128) < ROW_64_TILES) return tile_count(N, V, 64) <= 256 ? ROW_64_DEEP : ROW_64;
-  return N > 128 && tile_count(N, V, 256) >= LOGITS_MIN_TILES ? ROW_256 : ROW_128;
+// Which kernel a product of N tokens with V rows of W takes: the one that costs least, in ns, by what was measured:
+//   tiles   single ones (at most one a CU), else rounds of as many as the chip holds (64 x 64 and 128 x 128: two a CU; 256 x 256: one)
+//             64   3000 + 2.3 d (16 tokens, V 10000, d 512 .. 8192: 4.5, 5.5, 7.4, 12.5, 20.9 us)      round 2500 + 4.4 d ((100, 16032, 8192) 39.5)
+//            128   2000 + 6.8 d (6.6, 8.7, 12.9, 29.8, 56.3)                                          round 3000 + 8.4 d ((512, 33001, 4096) 109, (300, 128256, 4096) 231)
+//            256   11000 + 9.5 d a round ((600, 16032, 4096) 50.2, (256, 33001, 2048) 39.8, (200, 128256, 4096) 150)
+//           and never less than W's way from memory, 4000 + 5.8 TB/s; where that is what counts, 128 x 128 ((64, 128256, 4096) 64 / 128 / 256 126 / 108 / 118,
+//           (64, 50000, 8192) 99 / 82 / 100, (128, 33001, 4096) 52 / 47 / 51)
+//   direct  up to 16 tokens: 5200 (d up to 4096; 7100 at 8192) + 130 N, or 6000 + W at 6 TB/s and 3.5 % more a token: (1, 33001, 4096) 29 (64 / 128: 38 / 34),
+//           (16, 1000, 8192) 10.4 (18), (1, 128256, 4096) 93 (105 / 96), (16, 16032, 8192) 40 (24).  Log-probs: its partials, 16 rows each, cost 3.5 ns
+//           a tile in the merge
+enum RowTile { ROW_DIRECT, ROW_64, ROW_128, ROW_256 };
+constexpr int64_t ROW_64_MOST = 512;                 // 64 x 64 only below so many tiles of 128 x 128
+LLAMARL_RULE int64_t row_rounds(int64_t tiles, int64_t at_once, int64_t single, int64_t round) {
+  return tiles <= 256 ? single : (tiles + at_once - 1) / at_once * round;
 }
-// rows of W that a tile of partials has
-LLAMARL_RULE int row_tile_rows(RowTile t, int64_t d) {
-  const int direct = DIRECT_WAVES / direct_parts(d) * 16;
-  return t == ROW_256 ? 256 : t == ROW_128 ? 128 : t >= ROW_64_DEEP ? 64 : direct < 64 ? direct : 64;
+LLAMARL_RULE int64_t row_cost(RowTile t, int64_t N, int64_t V, int64_t d, bool logprobs) {
+  const int64_t memory = V * d / 5800 + 4000, never = (int64_t)1 << 60;
+  int64_t c = 0;
+  if (t == ROW_DIRECT) {
+    if (N > DIRECT_TOKENS) return never;
+    const int64_t least = (d <= 4096 ? 5200 : 3300 + d * 19 / 41) + 130 * N, stream = V * d / 100 * (200 + 7 * (N - 1)) / 12000 + 6000;
+    return (least > stream ? least : stream) + (logprobs ? V * 7 / 32 : 0);
+  }
+  if (t == ROW_64) c = tile_count(N, V, 128) < ROW_64_MOST ? row_rounds(tile_count(N, V, 64), 512, 3000 + d * 23 / 10, 2500 + d * 22 / 5) : never;
+  if (t == ROW_128) c = row_rounds(tile_count(N, V, 128), 512, 2000 + d * 34 / 5, 3000 + d * 42 / 5);
+  if (t == ROW_256) c = row_rounds(tile_count(N, V, 256), 256, 11000 + d * 19 / 2, 11000 + d * 19 / 2);
+  return c > memory ? c : memory;
 }
-// Logits: the first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind on tiles of `rest` in a launch of their own, by what
-// rounds of the grid cost (block_logits).
-struct RowLogits {
+LLAMARL_RULE RowTile row_tile(int64_t N, int64_t V, int64_t d, bool logprobs) {
+  RowTile best = ROW_128;
+  for (int t = ROW_DIRECT; t <= ROW_256; ++t)
+    if (row_cost((RowTile)t, N, V, d, logprobs) < row_cost(best, N, V, d, logprobs)) best = (RowTile)t;
+  return best;
+}
+// The first `rows` rows of W (all, or a multiple of 256) on tiles of `tile`, those behind the whole rounds of 256 x 256 ones on tiles of `rest` in a launch
+// of their own where that costs less: (1900, 33001, 2048) 169 / 137 us, (512, 33001, 4096) 120 / 80.
+struct RowPlan {
   RowTile tile;
   int64_t rows;
   RowTile rest;
 };
-LLAMARL_RULE RowLogits row_logits(int64_t N, int64_t V, int64_t d) {
-  const RowTile t = row_tile(N, V);
-  if (N <= FEW_TOKENS || t < ROW_128) return {t, V, t};
-  const int64_t tiles_t = (N + 255) / 256, tiles = tile_count(N, V, 256), rows = tiles / 256 * 256 / tiles_t * 256;
-  const int64_t round = (14000 + 25 * d / 2) * (4 * tiles_t - ((N - 1) % 256 < 128)) / (4 * tiles_t);
-  RowLogits best = {ROW_128, V, ROW_128};
-  int64_t cost = block_cost_128(N, V, d);
-  const int64_t whole = (tiles + 255) / 256 * round;
-  if (whole < cost) {
-    best.tile = ROW_256;
-    cost = whole;
-  }
-  if (rows > 0 && rows < V && tiles / 256 * round + block_cost_128(N, V - rows, d) + 3000 < cost)
-    best = {ROW_256, rows, tile_count(N, V - rows, 128) < ROW_64_TILES ? ROW_64 : ROW_128};
+LLAMARL_RULE RowPlan row_plan(int64_t N, int64_t V, int64_t d, bool logprobs) {
+  const RowTile t = row_tile(N, V, d, logprobs);
+  RowPlan best = {t, V, t};
+  const int64_t tiles_t = (N + 255) / 256, rows = tile_count(N, V, 256) / 256 * 256 / tiles_t * 256;
+  if (rows <= 0 || rows >= V || t == ROW_DIRECT) return best;
+  RowTile rest = row_tile(N, V - rows, d, logprobs);
+  if (rest == ROW_DIRECT) rest = ROW_64;
+  if (row_cost(ROW_256, N, rows, d, logprobs) + row_cost(rest, N, V - rows, d, logprobs) < row_cost(t, N, V, d, logprobs)) best = {ROW_256, rows, rest};
   return best;
 }
-// Floats of a plane of partials that serves any call of up to N tokens and V rows, see block_partials.
+// rows of W that a tile of partials has
+LLAMARL_RULE int row_tile_rows(RowTile t, int64_t d) {
+  const int direct = DIRECT_WAVES / direct_parts(d) * 16;
+  return t == ROW_256 ? 256 : t == ROW_128 ? 128 : t == ROW_64 ? 64 : direct < 64 ? direct : 64;
+}
+// Floats of a plane of partials that serves any call of up to N tokens and V rows: tiles of 128 rows or more, 64-row ones of fewer than ROW_64_MOST of 128 x
+// 128 (each two rows of partials of 128 tokens), or both behind one another; 16-row ones of up to 16 tokens.
 LLAMARL_RULE int64_t row_partials(int64_t N, int64_t V) {
   const int64_t n_pad = (N + 63) / 64 * 64;
-  const int64_t large = (V + 127) / 128 * n_pad, small = (V + 63) / 64 * n_pad, few = (V + 15) / 16 * 64;
-  const int64_t most = 256 * ROW_64_TILES, s = small < most ? small : most;
-  return large > few ? (large > s ? large : s) : few > s ? few : s;
+  const int64_t tiles = ((V + 127) / 128 + 1) * n_pad, small = ((V + 63) / 64 + 1) * n_pad, most = tiles + 256 * ROW_64_MOST, few = (V + 15) / 16 * 64;
+  const int64_t s = small < most ? small : most;
+  return s > few ? s : few;
 }
 
 }  // namespace llamarl

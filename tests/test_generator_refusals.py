@@ -78,15 +78,6 @@ def test_workspace_of_the_largest_call_serves_smaller_ones():
         last = b
 
 
-@pytest.mark.parametrize("N", [1, 5, 16, 17, 64, 65, 128, 129, 300, 1900, 16384])
-def test_partials_fit_their_planes(N):
-    rules = L._load_native()
-    for V in (1, 63, 64, 100, 1000, 5003, 8191, 16032, 32641, 33001, 128256, (1 << 21) - 1):
-        for d in (16, 512, 1040, 8192):
-            kernel, rows, floats = rules.row_plan(N, V, d)
-            assert -(-V // rows) * (-(-N // 64) * 64) <= floats, (N, V, d, kernel)
-
-
 @no_gpu_only
 def test_rms_norm(clib):
     def call(x=A, res=2 * A, w=3 * A, N=10, d=64, dt=L.BF16, w_dt=L.BF16, eps=1e-6, out=0, s=4 * A, h=5 * A, scale=None, rstd=7 * A):

@@ -71,7 +71,8 @@ def _cuda(*xs):
 # (N, V, d): every kernel is among them, see test_row_rules.py
 PRODUCTS = [(1, 5, 16), (1, 1000, 4096), (2, 300, 8208), (7, 1031, 528), (16, 4000, 1040), (16, 130, 48), (17, 70, 16), (33, 1000, 528), (48, 5003, 2064),
             (64, 64, 4096), (129, 600, 272), (300, 2000, 1040), (40, 30000, 272), (64, 17000, 1168), (128, 9000, 144), (65, 33001, 144), (128, 40000, 528),
-            (100, 33000, 272), (513, 8200, 208), (300, 33001, 528), (1300, 9000, 1168), (257, 50000, 144), (3000, 5003, 272), (1900, 33001, 272)]
+            (100, 33000, 272), (513, 8200, 208), (300, 33001, 528), (1300, 9000, 1168), (257, 50000, 144), (3000, 5003, 272), (200, 66001, 528), (300, 50000, 784),
+            (9, 33001, 1040), (3, 33001, 2064)]
 
 
 @pytest.mark.parametrize("N,V,d", PRODUCTS)
