@@ -522,13 +522,13 @@ llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* w
  * so the tokens are distributed as the policy's own, whatever the drafts are.  The last token is the first v, in the order of the vocabulary,
  * with  sum_{w <= v} r(w) > u_K sum_w r(w), r what it is drawn from.  T = 0: p_i is all on the largest logit (the first of equal ones), and so is q_i on x_i.
  * Distributions, sums and comparisons are in 64 bits.
- *   logits        in  [B,K+1,V] of type dt; rows behind a sequence's last place are not read
+ *   logits        in  [B,K+1,V] of type dt; rows behind a sequence's last place do not matter
  *   draft_logits  in  [B,K,V] of type dt, or NULL
  *   drafts        in  int32 [B,K] (may be NULL for K = 0);  one outside the vocabulary is refused, q_i has nothing on it then
  *   draft_lens    in  int32 [B] or NULL (= K); taken as 0 where it is less and as K where it is more
  *   temperature   in  float [B] or NULL (= 1)
- *   uniforms      in  float [B,K+1]; the last one of a sequence draws its token.  Numbers below 0 count as 0, one that is 1 or more accepts
-                    nothing of p_i <= q_i and draws the last token of r; NaN accepts nothing and draws the first
+ *   uniforms      in  float [B,K+1]; the last one of a sequence draws its token.  Numbers below 0 count as 0; one of 1 or more is compared as it
+ *                     is, and draws the last token of r; NaN accepts nothing, and draws the first
  *   tokens        out int32 [B,K+1]: accepted drafts, the token behind them, -1 from there on
  *   accepted      out int32 [B]
  *   logp          out float [B,K+1]: log p_i of the tokens (the generator's mu; 0 at T = 0), 0 from there on

@@ -146,6 +146,9 @@ def test_scales_that_are_not_finite(lib, N, V):
     ws[V // 2] = np.nan
     hs[1] = hs[3] = 0.5
     assert _same(lib.logits_rows(*_cuda(H, hs, W, ws)), row_logits(H, hs, W, ws))
+    logp, lse = lib.token_logprobs_rows(*_cuda(H, hs, W, ws, targets, mask))                # a distribution with a NaN in it is none
+    on = mask != 0
+    assert np.isnan(f64(lse))[on].all() and np.isnan(f64(logp))[on].all() and float(lse[3]) == 0
 
 
 def test_on_another_stream_and_in_a_graph(lib):

@@ -37,7 +37,7 @@ def _check(got, z, y, drafts, u, lens, temps):
 
 
 SIZES = [(1, 0, 1), (1, 0, 7), (1, 1, 1), (3, 2, 5), (7, 3, 5003), (2, 4, 8192), (2, 4, 8193), (4, 8, 20011), (64, 5, 1000), (1, 4, 128256), (5, 127, 33),
-         (1025, 1, 17), (2, 17, 40000)]
+         (1025, 1, 17), (2, 17, 40000), (2, 2, 140001), (1, 1, 700001)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -85,10 +85,29 @@ def test_drafts_of_the_target_itself_are_all_accepted(lib):
     assert got[1][0] == 0 and int(got[0][0, 0]) >= 0 and (got[1][1:] == 4).all()
 
 
+@pytest.mark.parametrize("V", [5, 333, 9001])
 @pytest.mark.parametrize("T", [-1.0, float("nan"), float("inf"), 1e-30, 1e-3, 1e30])
-def test_temperatures(lib, T):
-    z, y, drafts, u, lens, temps = _inputs(6, 3, 333, torch.float32, 9)
+def test_temperatures(lib, T, V):
+    z, y, drafts, u, lens, temps = _inputs(6, 3, V, torch.float32, 9)
     temps[:] = np.float32(T)
+    _check(_run(lib, z, y, drafts, u, lens, temps), z, y, drafts, u, lens, temps)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [300, 9001])
+def test_masks_of_the_lowest_number(lib, V, dtype):
+    """the type's lowest number is a token that is never drawn, unless a row holds nothing else; logits as large as the type's come out as T = 0 does"""
+    z, y, drafts, u, lens, temps = _inputs(12, 2, V, dtype, 21, greedy=0.0)
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z[:, :, :V // 3] = low
+    y[:, :, V // 2:] = low
+    z[2], y[3] = low, low
+    z[4] = -float("inf")
+    z[4, :, 7:20] = low
+    z[5, 0, V // 2], z[6, 1] = high, high
+    lens[:] = 2
+    _check(_run(lib, z, y, drafts, u, lens, temps), z, y, drafts, u, lens, temps)
+    z[:, :, :V // 3] = torch.where(torch.isinf(z[:, :, :V // 3]), z[:, :, :V // 3], torch.full((), -1e4, dtype=dtype))      # far enough
     _check(_run(lib, z, y, drafts, u, lens, temps), z, y, drafts, u, lens, temps)
 
 
