@@ -7,8 +7,9 @@
 //   k_rms_norm_bwd   dx, and the rows' share of dw in one partial row a workgroup
 //   k_norm_dw        those summed, in order
 //
-// Bound by memory: a row is read once, kept in registers until its norm is known, and written once.  Squares are summed in 64 bits: none
-// overflows or vanishes, and no order of the sum shows.
+// Bound by memory: a row is read once, kept in registers until its norm is known, and written once.  16384 x 4096 bf16 with a residual: forward 83 us (6.4
+// TB/s), backward 105 - 112 (4.8) and 5 for dw; 1900 x 8192 to e4m3 20 us; one row of 4096 2.5.  Squares are summed in 64 bits: none overflows or
+// vanishes, and no order of the sum shows.
 #pragma once
 #include "block_kernels.h"
 #include "row_kernels.h"
@@ -243,7 +244,7 @@ __device__ __forceinline__ void norm_columns(const NormBwdArgs& a, int block) {
   if (a.dw_bf16) static_cast<uint16_t*>(a.dw)[block * NORM_COLUMNS + c] = float_to_bf16_bits(t);
   else static_cast<float*>(a.dw)[block * NORM_COLUMNS + c] = t;
 }
-// Workgroups of 256 to 1024 threads walk over the rows, TH threads a row, the columns' share of dw in registers; its sums of a workgroup meet in LDS.
+// Workgroups of 256 to 1024 threads walk over the rows, TH threads a row, the next row on its way (1900 x 8192: 34 -> 24 us, with 256 workgroups for 1024), the columns' share of dw in registers; its sums of a workgroup meet in LDS.
 // Two workgroups a CU (one of 1024 threads): what a workgroup leaves of dw is written and read again, 4 d bytes each.
 constexpr int NORM_BWD_BLOCKS = 512;
 template <typename T, int TH, int UNITS>
