@@ -512,30 +512,31 @@ __device__ __forceinline__ int lane_behind(double sum, double own, double at) {
 }
 
 // Bound by latency: trips to memory one after the other, and the code itself, which a kernel this short fetches as it goes; so there is one place where
-// logits become r, passed VERIFY_UNITS times for a chunk's sums and once more for the part that the token is in.
+// logits become r, passed for each unit of a workgroup's and once more for the part that the token is in.  A sequence's units are dealt out to as many
+// workgroups as run at once (one sequence: 63 of one unit, 16 of four took 4 us more).
 template <typename T>
-__global__ __launch_bounds__(VERIFY_THREADS, 2) void k_verify_pick(VerifyArgs a) {
+__global__ __launch_bounds__(VERIFY_THREADS, 2) void k_verify_pick(VerifyArgs a, int units, int some) {
   constexpr int WAVES = VERIFY_THREADS / 64, PARTS = VERIFY_CHUNK / VERIFY_PART;
   __shared__ VerdictMemory memory;
   __shared__ int s_token;
   __shared__ float s_logit;
   __shared__ double s_sums[PARTS];
-  const int b = blockIdx.x / (unsigned)a.chunks, chunk = blockIdx.x - b * a.chunks, lane = threadIdx.x & 63, wave = wave_id();
+  const int groups = (units + some - 1) / some, b = blockIdx.x / (unsigned)groups, group = blockIdx.x - b * groups, lane = threadIdx.x & 63, wave = wave_id();
   const Verdict d = verdict_of(a, b, memory);
   int token = -1;
   if (d.none || d.temp == 0.f) {                     // uniform
-    if (chunk != 0) return;
+    if (group != 0) return;
     if (!d.none) token = d.first;
   } else {
     Rest<T> rest(a, b, d);
     const int parts = (int)((a.V + VERIFY_PART - 1) / VERIFY_PART), each = (parts + 63) / 64;
-    const bool alone = a.chunks == 1;
+    const bool alone = groups == 1 && units <= VERIFY_UNITS;
     double* sums = a.sums + (int64_t)b * a.chunks * PARTS;
     auto sum_at = [&](int i) { return alone ? s_sums[i] : __hip_atomic_load(sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     const float given = a.u[(int64_t)b * (a.K + 1) + a.K];
     const double u = fmin(fmax((double)given, 0.0), 0x1.fffffep-1);
-    // unit `at` of the row, 2048 tokens: a chunk's, then (turn 1) every one, by one workgroup, where p - q leaves nothing and it is p that is drawn from
-    int at = chunk * VERIFY_UNITS, end = at + VERIFY_UNITS;
+    // unit `at` of the row, 2048 tokens: `some` of them, then (turn) every one, by one workgroup, where p - q leaves nothing and it is p that is drawn from
+    int at = group * some, end = min(at + some, units);
     bool turn = false, last = false;
     double left = 0.0;
     int64_t v = ((int64_t)at * VERIFY_THREADS + threadIdx.x) * OPT_ITEMS;
@@ -589,8 +590,8 @@ __global__ __launch_bounds__(VERIFY_THREADS, 2) void k_verify_pick(VerifyArgs a)
       if (++at < end) continue;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      if (!turn && !alone) {
-        if (threadIdx.x == 0) s_token = __hip_atomic_fetch_add(a.ticket + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.chunks - 1u;
+      if (!turn && groups > 1) {
+        if (threadIdx.x == 0) s_token = __hip_atomic_fetch_add(a.ticket + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)groups - 1u;
         __syncthreads();
         if (!s_token) return;                        // uniform
         __syncthreads();
@@ -614,7 +615,7 @@ __global__ __launch_bounds__(VERIFY_THREADS, 2) void k_verify_pick(VerifyArgs a)
         rest.y = nullptr;
         rest.x = -1;
         at = 0;
-        end = a.chunks * VERIFY_UNITS;
+        end = units;
         v = (int64_t)threadIdx.x * OPT_ITEMS;
         z.load(rest.z, v, a.V);
         continue;
