@@ -811,7 +811,7 @@ PyObject* verify_drafts(PyObject* const* a) {
   const CallStream st(a[7], z);
   const at::Tensor tokens = fresh(z, {B, K + 1}, at::kInt), accepted = fresh(z, {B}, at::kInt), logp = fresh(z, {B, K + 1});
   const at::Tensor ws = workspace(a[6], llamarl_verify_drafts_workspace_bytes(B, K, V), z);
-  on_device_of(ws.is_cuda() ? ws : at::Tensor(), z, "ws", "logits");
+  on_device_of(ws, z, "ws", "logits");               // no host memory: it holds a counter
   check(unlocked([&] {
     return llamarl_verify_drafts(ptr(z), K > 0 ? ptr(y) : nullptr, ptr<int32_t>(drafts), ptr<int32_t>(lens), ptr<float>(temperature), ptr<float>(u), B, K,
                                  V, dt, ptr<int32_t>(tokens), ptr<int32_t>(accepted), ptr<float>(logp), ptr(ws), (size_t)ws.nbytes(), st.handle);

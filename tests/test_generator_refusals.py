@@ -161,7 +161,8 @@ def test_binding_refuses_shapes_types_and_strides(lib):
            lambda: lib.verify_drafts(z, d[:1], u), lambda: lib.verify_drafts(z[:, :2], d, u), lambda: lib.verify_drafts(z, d, u[:, :2]),
            lambda: lib.verify_drafts(z, d.long(), u), lambda: lib.verify_drafts(z, d, u, draft_logits=z), lambda: lib.verify_drafts(z, d, u, draft_lens=d),
            lambda: lib.verify_drafts(z, d, u, draft_logits=torch.zeros(2, 2, 9, **c)), lambda: lib.verify_drafts(z, d, u, temperature=s),
-           lambda: lib.verify_drafts(z.half(), d, u)]
+           lambda: lib.verify_drafts(z.half(), d, u), lambda: lib.verify_drafts(z, d, u, ws=torch.zeros(4096, dtype=torch.uint8)),
+           lambda: lib.verify_drafts(z, d, u, ws=torch.zeros(4096, dtype=torch.uint8, pin_memory=True))]
     for call in bad:
         with pytest.raises(lib.LlamarlError) as e:
             call()
