@@ -7,8 +7,8 @@
 //   k_rms_norm_bwd   dx, and the rows' share of dw in one partial row a workgroup
 //   k_norm_dw        those summed, in order
 //
-// Bound by memory: a row is read once, kept in registers until its norm is known, and written once.  16384 x 4096 bf16 with a residual: forward 83 us (6.4
-// TB/s), backward 105 - 112 (4.8) and 5 for dw; 1900 x 8192 to e4m3 20 us; one row of 4096 2.5.  Squares are summed in 64 bits: none overflows or
+// Bound by memory: a row is read once, kept in registers until its norm is known, and written once.  16384 x 4096 bf16 with a residual: forward 80 us (6.7
+// TB/s), backward 105 - 111 (4.9) and 5 for dw; 1900 x 8192 to e4m3 19 us; one row of 4096 2.5.  Squares are summed in 64 bits: none overflows or
 // vanishes, and no order of the sum shows.
 #pragma once
 #include "block_kernels.h"
@@ -44,16 +44,25 @@ __device__ __forceinline__ void load_unit(Raw8<float>& u, const void* p, int64_t
   if (left > 0) u.a = *reinterpret_cast<const f32x4_t*>(f);
   if (left >= OPT_ITEMS) u.b = *reinterpret_cast<const f32x4_t*>(f + 4);
 }
+// STREAM: past the caches, for s and dx, which nothing reads soon; h is read next and stays in them.  rms_norm with a residual and then a product with h, s cached
+// / past the caches / h past them as well: 16384 x 4096 181 / 176 / 184 us, 1900 x 8192 73 / 68 / 73, 64 x 4096 15.7 / 15.7 / 18.5.
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_word(void* p, const V& v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, static_cast<V*>(p));
+  else *static_cast<V*>(p) = v;
+}
+template <bool STREAM = false>
 __device__ __forceinline__ void store_unit(uint16_t* p, int64_t at, int left, const float (&o)[OPT_ITEMS]) {
   if (left < OPT_ITEMS) return;
   i32x4_t w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = (int)pack_bf16(o[2 * i], o[2 * i + 1]);
-  *reinterpret_cast<i32x4_t*>(p + at) = w;
+  store_word<STREAM>(p + at, w);
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store_unit(float* p, int64_t at, int left, const float (&o)[OPT_ITEMS]) {
-  if (left > 0) *reinterpret_cast<f32x4_t*>(p + at) = f32x4_t{o[0], o[1], o[2], o[3]};
-  if (left >= OPT_ITEMS) *reinterpret_cast<f32x4_t*>(p + at + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
+  if (left > 0) store_word<STREAM>(p + at, f32x4_t{o[0], o[1], o[2], o[3]});
+  if (left >= OPT_ITEMS) store_word<STREAM>(p + at + 4, f32x4_t{o[4], o[5], o[6], o[7]});
 }
 __device__ __forceinline__ void load_weights(const void* w, int bf16, int at, int left, float (&o)[OPT_ITEMS]) {
   if (bf16) {                                        // uniform
@@ -125,7 +134,7 @@ __global__ __launch_bounds__(NORM_THREADS_OF<TH>) void k_rms_norm(NormArgs a) {
       y[i].get(t);
 #pragma unroll
       for (int e = 0; e < OPT_ITEMS; ++e) s[i][e] += t[e];
-      store_unit(static_cast<T*>(a.sum), first + col, a.d - col, s[i]);
+      store_unit<true>(static_cast<T*>(a.sum), first + col, a.d - col, s[i]);
       if constexpr (sizeof(T) == 2) {                // as it is stored
 #pragma unroll
         for (int e = 0; e < OPT_ITEMS; e += 2) {
@@ -339,7 +348,7 @@ __global__ __launch_bounds__(NORM_THREADS_OF<TH>) void k_rms_norm_bwd(NormBwdArg
 #pragma unroll
         for (int e = 0; e < OPT_ITEMS; ++e) o[e] += t[e];
       }
-      store_unit(static_cast<T*>(a.dx), first + col, a.d - col, o);
+      store_unit<true>(static_cast<T*>(a.dx), first + col, a.d - col, o);
     }
   }
   if (a.part == nullptr) return;                     // uniform
