@@ -8,6 +8,7 @@ The upstream gradient of the loss is read by the kernels where autograd left it,
 csrc/native.cpp) also copies it to the host and refuses one that is not finite, but enqueues the kernels first: waiting
 for the copy before launching them left the GPU idle for the whole launch sequence (a third of a small model's step)."""
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as L
 
@@ -57,6 +58,7 @@ class _RmsNorm(torch.autograd.Function):
         return (h, s) if ctx.summed else h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_h, g_s=None):
         s, weight, rstd = ctx.saved_tensors
         if g_h is None:                      # the sum alone was used
@@ -68,7 +70,8 @@ class _RmsNorm(torch.autograd.Function):
 
 def rms_norm(x, weight, eps=1e-6, residual=None):
     """The norm in front of the head (`llamarl_rms_norm`): x, residual [..., d] and weight [d] (bf16 or fp32, contiguous, on the GPU) ->
-    h, or (h, x + residual) with a residual.  Gradients go to all three (`llamarl_rms_norm_bwd`)."""
+    h, or (h, x + residual) with a residual.  Gradients go to all three (`llamarl_rms_norm_bwd`), once: a gradient of a gradient is
+    refused."""
     shape = x.shape
     rows = x.reshape(-1, shape[-1])
     if residual is None:

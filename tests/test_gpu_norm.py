@@ -167,3 +167,13 @@ def test_autograd(lib, N, d, lead):
     assert np.abs(f64(x.grad) - want).max() <= 100 * U * np.abs(want).max() + 100 * U
     with torch.no_grad():
         assert torch.equal(rms_norm(x, w0, EPS), lib.rms_norm(x0, w0, EPS)[0])
+
+
+def test_a_gradient_of_a_gradient_is_refused(lib):
+    from paper_2505_24034_amd.autograd import rms_norm
+    x0, r0, w0, _, _ = _rows(3, 64, torch.float32, 13)
+    x, r, w = (t.clone().requires_grad_() for t in (x0, r0, w0))
+    h, s = rms_norm(x, w, EPS, residual=r)
+    dx, = torch.autograd.grad((h * h).sum() + (s * s).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        ((dx * dx).sum() + (x * x).sum()).backward()
