@@ -218,7 +218,7 @@ constexpr int VERIFY_ROWS_PER_CU = sizeof(T) == 2 ? 4 : 3;      // two chunks' l
 template <typename T>
 __global__ __launch_bounds__(VERIFY_THREADS, VERIFY_ROWS_PER_CU<T>) void k_verify_rows(VerifyArgs a, int each, int eager) {
   constexpr int WAVES = VERIFY_THREADS / 64;
-  __shared__ float s_m[WAVES];
+  __shared__ float s_m[2][WAVES];
   __shared__ double s_s[WAVES];
   __shared__ int s_i[WAVES];
   const int lane = threadIdx.x & 63, wave = wave_id(), groups = (a.chunks + each - 1) / each;
@@ -254,8 +254,13 @@ __global__ __launch_bounds__(VERIFY_THREADS, VERIFY_ROWS_PER_CU<T>) void k_verif
     a.part[row] = out;
     return;
   }
+  // A chunk has one barrier that every wavefront passes, between the maxima's writing and their reading; the second one only chunks with a sum or a first
+  // place have (none: nothing but -inf, a NaN, +inf).  So two chunks' maxima lie in turn in s_m: a wavefront writes a buffer again two chunks on, behind the
+  // barrier of the chunk between, which the others reach when they have read it.  s_s and s_i are written behind a chunk's first barrier, and so when all
+  // have read what the chunks before left there.
   for (int chunk = first_chunk; chunk < end; ++chunk) {
     const int64_t v0 = (int64_t)chunk * VERIFY_CHUNK;
+    float(&top)[WAVES] = s_m[chunk & 1];
     Logits8<T> x[VERIFY_UNITS];
     float m = -INFINITY;
 #pragma unroll
@@ -272,11 +277,11 @@ __global__ __launch_bounds__(VERIFY_THREADS, VERIFY_ROWS_PER_CU<T>) void k_verif
     }
     if (chunk + 1 < end) load_chunk(v0 + VERIFY_CHUNK);      // uniform
     m = wave_top_of(m);
-    if (lane == 0) s_m[wave] = m;
+    if (lane == 0) top[wave] = m;
     __syncthreads();
-    m = s_m[0];
+    m = top[0];
 #pragma unroll
-    for (int q = 1; q < WAVES; ++q) m = top_of(m, s_m[q]);
+    for (int q = 1; q < WAVES; ++q) m = top_of(m, top[q]);
     VerifyPart out = {__builtin_nan(""), m, 0x7fffffff};
     if (m < INFINITY) {                              // uniform; NaN is not
       out.sum = 0.0;
