@@ -890,6 +890,12 @@ PyObject* row_plan(PyObject* const* a) {
                        (long long)llamarl::row_partials(N, V));
 }
 
+// rows, B, V, CUs: chunks a workgroup and workgroups a row of k_verify_rows, units a workgroup and workgroups a sequence of k_verify_pick
+PyObject* verify_plan(PyObject* const* a) {
+  const llamarl::VerifyPlan p = llamarl::verify_plan(integer(a[0]), integer(a[1]), integer(a[2]), integer(a[3]));
+  return Py_BuildValue("LLLL", (long long)p.each, (long long)p.row_groups(), (long long)p.some, (long long)p.pick_groups());
+}
+
 template <PyObject* (*F)(PyObject* const*), int NARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -918,7 +924,7 @@ PyMethodDef g_methods[] = {
     ENTRY(offpolicy_loss_bwd, 13), ENTRY(offpolicy_loss_bwd_slice, 10), ENTRY(offpolicy_loss_bwd_device_scale, 9),
     ENTRY(group_advantages, 5), ENTRY(kl_shaped_rewards, 6), ENTRY(grad_norm, 4), ENTRY(adamw_step, 15), ENTRY(quantise_blocks, 3), ENTRY(logits_blocks, 7),
     ENTRY(token_logprobs_blocks, 8), ENTRY(quantise_rows, 2), ENTRY(logits_rows, 7), ENTRY(token_logprobs_rows, 8), ENTRY(rms_norm, 6),
-    ENTRY(rms_norm_bwd, 9), ENTRY(verify_drafts, 8), ENTRY(row_plan, 4), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
+    ENTRY(rms_norm_bwd, 9), ENTRY(verify_drafts, 8), ENTRY(row_plan, 4), ENTRY(verify_plan, 4), ENTRY(block_plan, 4), ENTRY(block_logits_plan, 3), ENTRY(tile_walk, 3), ENTRY(logits_width, 5), ENTRY(dz_columns, 2), ENTRY(logits_tile, 5), ENTRY(store_tile, 4), ENTRY(pair_workgroups, 5), {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

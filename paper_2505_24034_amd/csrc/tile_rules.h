@@ -422,4 +422,24 @@ LLAMARL_RULE int64_t row_partials(int64_t N, int64_t V) {
   return s > few ? s : few;
 }
 
+// ---- drafted tokens (verify_kernels.h) ---------------------------------------------------------------------------------------
+// How a call is dealt out on a chip of `cus` CUs.  Rows are cut into chunks of VERIFY_ROW_CHUNK logits, `each` neighbouring ones a workgroup: one where that
+// fills the chip no more than a few times over.  The row that a sequence's last token comes from is cut into units of VERIFY_PICK_UNIT, `some` of them a
+// workgroup: as few as let all workgroups run at once.
+constexpr int64_t VERIFY_ROW_CHUNK = 8192, VERIFY_PICK_UNIT = 2048;
+constexpr int64_t VERIFY_MOST_AT_ONCE = 8, VERIFY_MOST_EACH = 4, VERIFY_PICK_AT_ONCE = 2;
+struct VerifyPlan {
+  int64_t chunks, each, units, some;
+  LLAMARL_RULE int64_t row_groups() const { return (chunks + each - 1) / each; }      // workgroups of a row
+  LLAMARL_RULE int64_t pick_groups() const { return (units + some - 1) / some; }      // ... of a sequence
+};
+// rows: B (K + 1), and the drafts' B K where they have logits
+LLAMARL_RULE VerifyPlan verify_plan(int64_t rows, int64_t B, int64_t V, int64_t cus) {
+  VerifyPlan p = {(V + VERIFY_ROW_CHUNK - 1) / VERIFY_ROW_CHUNK, 1, (V + VERIFY_PICK_UNIT - 1) / VERIFY_PICK_UNIT, 1};
+  const int64_t each = rows * p.chunks / (cus * VERIFY_MOST_AT_ONCE), at_once = cus * VERIFY_PICK_AT_ONCE, some = (B * p.units + at_once - 1) / at_once;
+  p.each = each < 1 ? 1 : each > VERIFY_MOST_EACH ? VERIFY_MOST_EACH : each;
+  p.some = some > p.units ? p.units : some;
+  return p;
+}
+
 }  // namespace llamarl

@@ -21,17 +21,14 @@ bool verify_fits(int64_t B, int64_t K, int64_t V) {
   return B > 0 && K >= 0 && V > 0 && K <= VERIFY_MOST_DRAFTS && V < BLOCK_MOST_ROWS && B < (int64_t)1 << 20 &&
          B * (2 * K + 1) * ((V + VERIFY_CHUNK - 1) / VERIFY_CHUNK) < ((int64_t)1 << 32) / VERIFY_THREADS;
 }
-constexpr int VERIFY_MOST_AT_ONCE = 8, VERIFY_MOST_EACH = 4, VERIFY_PICK_AT_ONCE = 2;
+static_assert(VERIFY_ROW_CHUNK == VERIFY_CHUNK && VERIFY_PICK_UNIT == VERIFY_THREADS * OPT_ITEMS, "the rule's cuts");
 template <typename T>
 llamarl_status launch_verify(const VerifyArgs& a, int64_t rows, hipStream_t st) {
-  // Chunks of a workgroup: one where that fills the chip no more than a few times over, and then its logits are asked for before it knows whether
-  // somebody wants them.
-  const int64_t each = std::min<int64_t>(std::max<int64_t>(rows * a.chunks / persistent_grid((int64_t)1 << 30, VERIFY_MOST_AT_ONCE), 1), VERIFY_MOST_EACH);
-  k_verify_rows<T><<<dim3((unsigned)(rows * ((a.chunks + each - 1) / each))), dim3(VERIFY_THREADS), 0, st>>>(a, (int)each, each == 1);
+  const VerifyPlan p = verify_plan(rows, a.B, a.V, persistent_grid((int64_t)1 << 30));
+  // a workgroup's only chunk is asked for before it knows whether somebody wants it
+  k_verify_rows<T><<<dim3((unsigned)(rows * p.row_groups())), dim3(VERIFY_THREADS), 0, st>>>(a, (int)p.each, p.each == 1);
   HIP_TRY(hipGetLastError());
-  const int64_t units = (a.V + VERIFY_THREADS * OPT_ITEMS - 1) / (VERIFY_THREADS * OPT_ITEMS), at_once = persistent_grid((int64_t)1 << 30, VERIFY_PICK_AT_ONCE);
-  const int64_t some = std::min((a.B * units + at_once - 1) / at_once, units);
-  k_verify_pick<T><<<dim3((unsigned)(a.B * ((units + some - 1) / some))), dim3(VERIFY_THREADS), 0, st>>>(a, (int)units, (int)some);
+  k_verify_pick<T><<<dim3((unsigned)(a.B * p.pick_groups())), dim3(VERIFY_THREADS), 0, st>>>(a, (int)p.units, (int)p.some);
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }

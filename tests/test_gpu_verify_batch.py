@@ -8,10 +8,30 @@ from test_gpu_verify import _check, _inputs, _run
 
 pytestmark = pytest.mark.gpu
 CHUNK = 8192
+# What each of them reaches: see test_verify_rules.py.
+MASKED = [(64, 5, 45001, True), (128, 5, 45001, False), (256, 3, 40000, True)]
+BATCHES = [(300, 3, 17000, True), (600, 2, 5000, True), (700, 2, 8000, False), (600, 1, 9001, True), (1500, 1, 3000, True), (130, 0, 150001, False)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("B,K,V,model", [(64, 5, 45001, True), (128, 5, 45001, False), (256, 3, 40000, True)])
+@pytest.mark.parametrize("B,K,V,model", BATCHES)
+def test_batches(lib, B, K, V, model, dtype):
+    """ragged lengths, some at T = 0; every fourth sequence's drafts are the target's own, and where its first is outside the vocabulary nothing is left of
+    p - q: the token comes out of p"""
+    z, y, drafts, u, lens, temps = _inputs(B, K, V, dtype, B + V, model, size=4.0)
+    if model:
+        y[::4] = z[::4, :K]
+        drafts[::8, 0] = -1
+        lens[::8], temps[::8] = K, 0.9
+    got = _run(lib, z, y, drafts, u, lens, temps)
+    _check(got, z, y, drafts, u, lens, temps)
+    scratch = torch.full((lib.verify_drafts_workspace_bytes(B, K, V),), 255, dtype=torch.uint8, device="cuda")
+    again = _run(lib, z, y, drafts, u, lens, temps, ws=scratch)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,K,V,model", MASKED)
 def test_chunks_without_a_sum(lib, B, K, V, model, dtype):
     """neighbouring chunks of which nothing is left, between ones with logits; a NaN or an infinity in one chunk only"""
     z, y, drafts, u, lens, temps = _inputs(B, K, V, dtype, B + V, model, greedy=0.2, size=5.0)
