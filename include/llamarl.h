@@ -516,8 +516,8 @@ llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* w
  * or copied from the prompt), logits at each draft's place and at the one behind the last, and numbers u_0 .. u_K in [0, 1).  With
  * p_i = softmax(logits / T) and q_i = softmax(draft_logits / T), or q_i all on x_i without draft_logits:
  *     draft i is accepted while u_i q_i(x_i) < p_i(x_i)
- *     the first that is not is replaced by a token out of max(p_i - q_i, 0), normalised (out of p_i where that leaves less than
- *         2^-40, which is the rounding of p_i and q_i)
+ *     the first that is not is replaced by a token out of max(p_i - q_i, 0), normalised (out of p_i where that leaves no more than
+ *         2^-36: p_i and q_i are good to 5.3e-12 of themselves, so it may be nothing)
  *     behind n accepted drafts comes a token out of p_n
  * so the tokens are distributed as the policy's own, whatever the drafts are.  The last token is the first v, in the order of the vocabulary,
  * with  sum_{w <= v} r(w) > u_K sum_w r(w), r what it is drawn from.  T = 0: p_i is all on the largest logit (the first of equal ones), and so is q_i on x_i.

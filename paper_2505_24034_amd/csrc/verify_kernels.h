@@ -23,9 +23,10 @@ namespace llamarl {
 constexpr int VERIFY_THREADS = 256, VERIFY_UNITS = 4, VERIFY_CHUNK = VERIFY_THREADS * VERIFY_UNITS * OPT_ITEMS;      // logits of a workgroup
 constexpr int VERIFY_MOST_DRAFTS = 127;              // 2 K + 1 rows of a sequence
 constexpr int VERIFY_PART = 64 * OPT_ITEMS;          // ... of a wavefront's unit: what the sums that a token is looked up in are of
-// p and q carry 2^-53 of themselves, and there are up to 2^21 of them: what max(p - q, 0) leaves below this is their rounding.  A draft of q is refused
-// with the probability of that remainder, so p is drawn from instead.
-constexpr double REST_LEAST = 0x1p-40;
+// An entry of p is a power, times its row's scale, over a sum of powers times their chunk's two scales: five powers, each within 1.06e-12 of itself (exp2_parts).
+// So of equal distributions max(p - q, 0) leaves up to ten times that, 1.06e-11 (logits and the same plus a constant: 2.2e-12 seen), and what it leaves below
+// 2^-36 = 1.46e-11 is no distribution.  A draft of q is refused with the probability of that remainder, so p is drawn from instead.
+constexpr double REST_LEAST = 0x1p-36;
 
 // 2^f for |f| <= 1/2, within 1.1e-12 of it: interpolated at Chebyshev's nodes.  A token moves with the probability of its border's, 1e-7 over a vocabulary.
 // Several at once, operation by operation: a chain of dependent ones takes twice the time of its instructions where a SIMD has one or two wavefronts.
