@@ -527,8 +527,9 @@ llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* w
  *   drafts        in  int32 [B,K] (may be NULL for K = 0);  one outside the vocabulary is refused, q_i has nothing on it then
  *   draft_lens    in  int32 [B] or NULL (= K); taken as 0 where it is less and as K where it is more
  *   temperature   in  float [B] or NULL (= 1)
- *   uniforms      in  float [B,K+1]; the last one of a sequence draws its token.  Numbers below 0 count as 0; one of 1 or more is compared as it
- *                     is, and draws the last token of r; NaN accepts nothing, and draws the first
+ *   uniforms      in  float [B,K+1]; the last one of a sequence draws its token.  Numbers below 0 count as 0.  One of 1 or more is compared as it
+ *                     is, and draws what 1 - 2^-24, the largest float below 1, would: 1 is what 64-bit numbers next to it round to.  NaN and infinity
+ *                     accept nothing; NaN draws the first token of r
  *   tokens        out int32 [B,K+1]: accepted drafts, the token behind them, -1 from there on
  *   accepted      out int32 [B]
  *   logp          out float [B,K+1]: log p_i of the tokens (the generator's mu; 0 at T = 0), 0 from there on

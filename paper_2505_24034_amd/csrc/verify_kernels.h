@@ -540,7 +540,7 @@ __global__ __launch_bounds__(VERIFY_THREADS, 2) void k_verify_pick(VerifyArgs a,
     double* sums = a.sums + (int64_t)b * a.chunks * PARTS;
     auto sum_at = [&](int i) { return alone ? s_sums[i] : __hip_atomic_load(sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
     const float given = a.u[(int64_t)b * (a.K + 1) + a.K];
-    const double u = fmin(fmax((double)given, 0.0), 0x1.fffffep-1);
+    const double u = fmin(fmax((double)given, 0.0), 0x1.fffffep-1);      // 1 and more count as the largest fp32 number below 1
     // unit `at` of the row, 2048 tokens: `some` of them, then (turn) every one, by one workgroup, where p - q leaves nothing and it is p that is drawn from
     int at = group * some, end = min(at + some, units);
     bool turn = false, last = false;
