@@ -48,6 +48,12 @@ def aipo_loss(H, W, targets, mu_logp, adv, mask, rho=2.0, norm_mode=L.NORM_TOKEN
                            float(eps_lo), float(eps_hi), dW_dtype)
 
 
+def _gradient(g):
+    """g as the library takes it: dense, and 16-byte aligned, which a part of a larger gradient (of a concatenation, say) need not be"""
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
@@ -63,7 +69,7 @@ class _RmsNorm(torch.autograd.Function):
         s, weight, rstd = ctx.saved_tensors
         if g_h is None:                      # the sum alone was used
             return g_s, None, g_s if ctx.summed else None, None
-        dx, dw = L.rms_norm_bwd(g_h.contiguous(), s, weight, rstd, dsum=None if g_s is None else g_s.contiguous(),
+        dx, dw = L.rms_norm_bwd(_gradient(g_h), s, weight, rstd, dsum=None if g_s is None else _gradient(g_s),
                                 want_dweight=ctx.needs_input_grad[1])
         return dx, dw, dx if ctx.summed else None, None
 
