@@ -49,8 +49,9 @@ def aipo_loss(H, W, targets, mu_logp, adv, mask, rho=2.0, norm_mode=L.NORM_TOKEN
 
 
 def _gradient(g):
-    """g as the library takes it: dense, and 16-byte aligned, which a part of a larger gradient (of a concatenation, say) need not be"""
-    g = g.contiguous()
+    """g as the library takes it: dense, not a view that negates, and 16-byte aligned, which a part of a larger gradient (of a
+    concatenation, say) need not be"""
+    g = g.resolve_neg().contiguous()
     return g if g.data_ptr() % 16 == 0 else g.clone()
 
 

@@ -1,4 +1,4 @@
-"""Gradients as autograd hands them to the norm: parts of larger ones, which start anywhere, and one number spread out."""
+"""Gradients as autograd hands them to the norm: parts of larger ones, which start anywhere, views that negate, one number spread out."""
 import pytest
 import torch
 
@@ -26,6 +26,20 @@ def test_parts_of_a_larger_gradient(lib, lead, dtype):
     h, s = rms_norm(x, w, 1e-5, residual=r)
     want = torch.autograd.grad([h, s], leaves, [scale[lead:].view(5, 64).clone()] * 2)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_views_that_negate(lib):
+    from paper_2505_24034_amd.autograd import rms_norm
+    x, w, r = leaves = _leaves(torch.float32)
+    a, b = (torch.randn(5, 64, device="cuda") for _ in range(2))
+    dense = torch._neg_view(a)
+    strided = torch.complex(b, b).conj().imag
+    assert dense.is_neg() and dense.is_contiguous() and strided.is_neg()
+    h, s = rms_norm(x, w, 1e-5, residual=r)
+    got = torch.autograd.grad([h, s], leaves, [dense, strided])
+    h, s = rms_norm(x, w, 1e-5, residual=r)
+    want = torch.autograd.grad([h, s], leaves, [-a, -b])
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
 def test_a_gradient_of_one_number_spread_out(lib):
