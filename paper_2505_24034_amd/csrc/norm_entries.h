@@ -35,9 +35,10 @@ int row_threads(int64_t d) {
 }
 // rows of a workgroup
 int64_t rows_each(int64_t d) { return row_threads(d) == 64 ? 4 : 1; }
-llamarl_status check_row_launch(int64_t rows, int64_t d) {
-  const int threads = std::max(row_threads(d), 256);
-  return (rows + rows_each(d) - 1) / rows_each(d) * threads >= (int64_t)1 << 32 ? fail(LLAMARL_ERR_UNSUPPORTED, "too many rows") : LLAMARL_OK;
+// `rows` on `threads` threads each: a launch has fewer than 2^32
+llamarl_status check_row_launch(int64_t rows, int threads) {
+  const int64_t each = threads == 64 ? 4 : 1;
+  return (rows + each - 1) / each * std::max(threads, 256) >= (int64_t)1 << 32 ? fail(LLAMARL_ERR_UNSUPPORTED, "too many rows") : LLAMARL_OK;
 }
 
 llamarl_status check_norm(int64_t N, int64_t d, llamarl_dtype dt, llamarl_dtype w_dt, const void* w) {
@@ -47,7 +48,7 @@ llamarl_status check_norm(int64_t N, int64_t d, llamarl_dtype dt, llamarl_dtype 
   if (d > NORM_MOST_COLS) return fail(LLAMARL_ERR_UNSUPPORTED, "d must be at most %lld", (long long)NORM_MOST_COLS);
   if (N >= (int64_t)1 << 31) return fail(LLAMARL_ERR_UNSUPPORTED, "too many rows");
   if (!aligned16(w)) return fail(LLAMARL_ERR_INVALID_ARG, "weight must be 16-byte aligned");
-  return check_row_launch(N, d);
+  return check_row_launch(N, row_threads(d));
 }
 // workgroups, and rows of partial sums; none for few rows, whose columns are summed up as they are
 int64_t norm_bwd_blocks(int64_t N, int64_t d) {

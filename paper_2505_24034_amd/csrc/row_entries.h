@@ -70,10 +70,14 @@ llamarl_status launch_row_partials(const FwdArgs& a, const RowHead& x, hipStream
   HIP_TRY(hipGetLastError());
   return LLAMARL_OK;
 }
+constexpr int QUANTISE_MOST_THREADS = 1024;          // of rows longer than NORM_MOST_COLS
+int quantise_threads(int64_t cols) {
+  return cols > NORM_MOST_COLS ? QUANTISE_MOST_THREADS : with_quantise_shape(cols, [](auto s) { return decltype(s)::TH; });
+}
 template <typename T>
 void launch_quantise_int8(const QuantiseRowsArgs& a, hipStream_t st) {
   if (a.cols > NORM_MOST_COLS) {
-    k_quantise_int8<T, 1024, 0><<<dim3((unsigned)a.rows), dim3(1024), 0, st>>>(a);
+    k_quantise_int8<T, QUANTISE_MOST_THREADS, 0><<<dim3((unsigned)a.rows), dim3(QUANTISE_MOST_THREADS), 0, st>>>(a);
     return;
   }
   with_quantise_shape(a.cols, [&](auto s) {
@@ -92,7 +96,7 @@ llamarl_status llamarl_quantise_rows(const void* x, int64_t rows, int64_t cols, 
   if (!x || !q || !scale) return fail(LLAMARL_ERR_INVALID_ARG, "null pointer argument");
   if (!known(dt)) return fail(LLAMARL_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);
   llamarl_status s = check_row_matrix(rows, cols);
-  if (s == LLAMARL_OK) s = check_row_launch(rows, cols);
+  if (s == LLAMARL_OK) s = check_row_launch(rows, quantise_threads(cols));
   if (s != LLAMARL_OK) return s;
   if (!aligned16(x) || !aligned16(q)) return fail(LLAMARL_ERR_INVALID_ARG, "x and q must be 16-byte aligned");
   if (!aligned_to(scale, 4)) return fail(LLAMARL_ERR_INVALID_ARG, "scale must be 4-byte aligned");
