@@ -452,7 +452,7 @@ llamarl_status llamarl_token_logprobs_blocks(const void* H, const uint8_t* H_sca
  * the nearest integer (ties to even): -127 .. 127.  A row below 2^-100 is zeros, with scale 0; one with an entry that is not finite is
  * zeros with scale NaN.
  *   x      in  [rows,cols] of type dt, dense; cols % 16 == 0, cols < 2^17; q: out int8 [rows,cols]; scale: out float [rows].  x and q 16-byte
- *              aligned; none may overlap another
+ *              aligned; none may overlap another.  At most 2^26 - 4 rows of up to 1024 columns, 2^24 - 1 of up to 8192, 2^22 - 1 of more
  */
 llamarl_status llamarl_quantise_rows(const void* x, int64_t rows, int64_t cols, llamarl_dtype dt, int8_t* q, float* scale, void* stream);
 
@@ -461,7 +461,7 @@ llamarl_status llamarl_quantise_rows(const void* x, int64_t rows, int64_t cols, 
  *     z[t,v] = (sum_k H[t,k] W[v,k]) * W_scale[v] * H_scale[t]
  * The sum is exact; it is rounded to fp32, multiplied twice, and rounded once more for bf16.
  *   H, H_scale  in  int8 [N,d], float [N];  d % 16 == 0, d < 2^17, N * d < 2^31
- *   W, W_scale  in  int8 [V,d], float [V];  V < 2^21
+ *   W, W_scale  in  int8 [V,d], float [V];  V < 2^21, ceil(N / 64) * ceil(V / 64) < 2^31
  *   z           out [N,V] of type z_dt; apart from the operands
  */
 llamarl_status llamarl_logits_rows(const int8_t* H, const float* H_scale, const int8_t* W, const float* W_scale, int64_t N, int64_t d,
@@ -483,6 +483,7 @@ llamarl_status llamarl_token_logprobs_rows(const int8_t* H, const float* H_scale
  * Without a residual (NULL, as sum then is) it is x that is normalised.  Squares are summed in 64 bits, the rest is fp32; the norm is that of
  * the sum as it is stored.
  *   x, residual  in  [N,d] of type dt;  d at most 16384, a multiple of 8 (bf16) or 4 (fp32), of 16 for an output in 8 bits
+ *                    N at most 2^26 - 4 for d up to 1024, 2^24 - 1 up to 2048, 2^23 - 1 up to 4096, 2^22 - 1 beyond
  *   weight       in  [d] of type w_dt
  *   eps          positive
  *   out          h is of type dt (h_scale NULL), or in 8 bits: what llamarl_quantise_blocks (block_rows 1; h_scale as there) or
@@ -499,7 +500,7 @@ llamarl_status llamarl_rms_norm(const void* x, const void* residual, const void*
  * Its backward.  With n = s * rstd and g = dh * weight:
  *     dx = rstd * (g - n * mean(g * n)) + dsum            dweight = sum over rows of dh * n
  * dx is the gradient of x and of the residual alike; dsum what comes back to the sum itself.
- *   dh, dsum  in  [N,d] of type dt; dsum may be NULL (= 0)
+ *   dh, dsum  in  [N,d] of type dt, N and d as there; dsum may be NULL (= 0)
  *   s         in  [N,d]: what was normalised (sum, or x without a residual);  rstd: in float [N]
  *   dx        out [N,d] of type dt
  *   dweight   out [d] of type dw_dt, or NULL: ws is not needed then
@@ -535,7 +536,8 @@ llamarl_status llamarl_rms_norm_bwd(const void* dh, const void* s, const void* w
  *   logp          out float [B,K+1]: log p_i of the tokens (the generator's mu; 0 at T = 0), 0 from there on
  *   ws            scratch, >= llamarl_verify_drafts_workspace_bytes(B, K, V), which falls with none of them
  * A logit of -inf is a token that is never drawn.  A row without a distribution (a NaN, an infinite or nothing but -inf logits; T negative or not
- * finite) accepts no draft, and if it is the last one's, its token is -1 and its logp NaN.  K is at most 127, B < 2^20, V < 2^21.
+ * finite) accepts no draft, and if it is the last one's, its token is -1 and its logp NaN.  K is at most 127, B < 2^20, V < 2^21,
+ * B (2 K + 1) ceil(V / 8192) < 2^24.
  * Outputs and ws overlap no other array (INVALID_ARG).
  */
 size_t llamarl_verify_drafts_workspace_bytes(int64_t B, int64_t K, int64_t V);
