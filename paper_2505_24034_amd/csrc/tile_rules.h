@@ -366,7 +366,7 @@ LLAMARL_RULE int64_t block_partials(int64_t N, int64_t V) {
 //           (64, 50000, 8192) 99 / 82 / 100, (128, 33001, 4096) 52 / 47 / 51)
 //   direct  up to 16 tokens: 5200 (d up to 4096; 7100 at 8192) + 130 N, or 6000 + W at 6 TB/s and 3.5 % more a token: (1, 33001, 4096) 29 (64 / 128: 38 / 34),
 //           (16, 1000, 8192) 10.4 (18), (1, 128256, 4096) 93 (105 / 96), (16, 16032, 8192) 40 (24).  Log-probs: its partials, 16 rows each, cost 3.5 ns
-//           a tile in the merge
+//           a tile in the merge.  On tiles they are put at what logits take, and a single round takes longer: (580 of 1041, 5003, 528) on 128 x 128 11.2 for 5.6
 enum RowTile { ROW_DIRECT, ROW_64, ROW_128, ROW_256 };
 constexpr int64_t ROW_64_MOST = 512;                 // 64 x 64 only below so many tiles of 128 x 128
 LLAMARL_RULE int64_t row_rounds(int64_t tiles, int64_t at_once, int64_t single, int64_t round) {

@@ -13,7 +13,7 @@
 //
 // Everything that decides is in 64 bits: a token is one of V borders, and with fp32's 1e-7 in each of 128256 terms every tenth sample would have
 // moved by a token.  fp64 runs at fp32's rate here, so a logit costs what its instructions are, whatever their width: see PowersOf.
-// 64 sequences with up to five drafts over 128256 bf16 logits: 46 + 29 us, half of the first at the rate of vector instructions (memory: 17); one sequence with
+// 64 sequences with up to five drafts over 128256 bf16 logits: 46 - 48 + 29 - 30 us, half of the first at the rate of vector instructions (memory: 17); one sequence with
 // four: 4.8 + 9.7, trips to memory.
 #pragma once
 #include "norm_kernels.h"
